@@ -390,6 +390,7 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
                 for (int i = 0; i < 16; ++i) O[db][i] = f * O[db][i] + f_other * other[64 * (16 * db + i)];
             m_run = m;
         }
+        lds_handover();                            // the reads are in front of the outputs that pass through the same bytes
     }
     // ---- normalise and store, or leave a share (as the tile kernels over a bf16 cache do)
     if (item.part >= 0) {
@@ -409,7 +410,7 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
         return;
     }
     if (wave_live) {
-        // (of another wavefront's sums nobody reads here any more: in SPLIT a wavefront's place covers its own group's sums only in part)
+        // (in SPLIT a wavefront's place is that of its own group's sums, which other lanes have read)
         store_rows<D>(a, q0, g, G, item.row0 + group * 32, row_last, smem + group * (SPLIT ? 64 * (D / 2 + 2) * 4 : QueryRows<D, STYLE>::kQueryBytes), O, 1.f / l_all);
     }
 }

@@ -75,3 +75,38 @@ def test_shares_are_merged_with_their_loads_in_one_block():
         loads = [len(re.findall(r"= load float, ptr addrspace\(1\)", block)) for block in re.split(r"\n\d+:", body)]
         loads = [n for n in loads if n]
         assert sorted(loads) == [2 * 4] * 4 + [4 * 4] * 4           # maxima and denominators, then four sums each, of four times four shares
+
+
+def lds_accesses(body):
+    """stores, loads, transposing reads and what orders them, in the order of the text"""
+    kinds = [("store", r"\bstore .*ptr addrspace\(3\)"), ("tr", r"ds\.read\.tr.*ptr addrspace\(3\)"), ("load", r"\bload .*ptr addrspace\(3\)"),
+             ("fence", r"\bfence "), ("barrier", r"llvm\.amdgcn\.s\.barrier\(")]
+    return [kind for line in body.splitlines() for kind, text in kinds if re.search(text, line) and not line.startswith("declare")]
+
+
+def test_the_tile_kernels_of_the_4_bit_cache_hand_their_outputs_on_behind_fences():
+    """Behind the last barrier a wavefront of the 128-row kernel reads the sums of the one that had the other half of the keys, and hands its rows
+    on through the same bytes, to other lanes: reads and writes of different types and lanes, which only a fence keeps in their order."""
+    kernels = re.findall(r"define [^\n]*amdgpu_kernel void @([^\n(]*attn_kv4_tiles_kernel[^\n(]*)(.*?\n})", intermediate(os.path.join(CSRC, "ca_attn_kv4_tiles.hip")), re.S)
+    assert len(kernels) == 8
+    for name, body in kernels:
+        seen = lds_accesses(body)
+        tail = seen[len(seen) - seen[::-1].index("barrier"):]
+        turns = [kind for i, kind in enumerate(tail) if i == 0 or kind != tail[i - 1]]
+        turns = turns[turns[0] == "fence":]
+        assert turns == (["load", "fence"] if "Lb1E" in name else []) + ["store", "fence", "load"], name
+
+
+def test_the_few_rows_kernel_of_the_4_bit_cache_reads_its_values_behind_fences():
+    """A wavefront writes its values to LDS and reads them transposed, step after step, without a barrier."""
+    kernels = re.findall(r"define [^\n]*amdgpu_kernel void @[^\n]*attn_kv4_kernel.*?\n}", intermediate(os.path.join(CSRC, "ca_attn_kv4.hip")), re.S)
+    assert len(kernels) == 4
+    for body in kernels:
+        seen = lds_accesses(body)
+        reads = [i for i, kind in enumerate(seen) if kind == "tr"]
+        assert len(reads) >= 8
+        writes = [i for i, kind in enumerate(seen) if kind == "store"]
+        for access, others in ((reads, writes), (writes, reads)):
+            for i in access:
+                before = [j for j in others if j < i]
+                assert not before or {"fence", "barrier"} & set(seen[before[-1]:i]), (i, before[-1])

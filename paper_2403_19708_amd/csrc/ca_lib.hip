@@ -1486,6 +1486,7 @@ ca_status ca_rope_rebase(ca_ctx *ctx, const ca_batch *b, void *stream_) {
             ctx->pipelined = ctx->prerotate && ctx->v_t && !ctx->kv4 && tile == 256 && c.attn_variant != 3 && c.attn_variant != 1;
         }
         const auto lay_out = [&](int tile, double *us) -> ca_status {
+        ctx->last_round_cut = false;        // (of this layout, whatever one that is not taken did)
         {
             size_t dense_pages = 0;
             if (ctx->prerotate)

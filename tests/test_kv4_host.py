@@ -6,6 +6,7 @@ import pytest
 
 import kv4_oracle as o4
 import paper_2403_19708_amd as ca
+from hip_model import Turn, in_model
 from paper_2403_19708_amd import binding
 from synth import bf16_bits_to_f64, draw_values_bf16
 
@@ -75,3 +76,51 @@ def test_calls_without_a_context():
     assert lib.ca_kv_read_layer(None, 0, None, None, None, None, None, None, None) == 1
     assert lib.ca_head_norm_set(None, 0, None, None, 1e-6, None) == 1
     assert {"ca_create_kv4", "ca_kv_sizes", "ca_kv_read_layer", "ca_head_norm_set"} <= set(binding.SYMBOLS)
+
+
+# ---- on the model of the HIP runtime ------------------------------------------------------------------------------------------------
+class Turn4(Turn):
+    """hip_model's batch over a 4-bit cache"""
+
+    def __init__(self, m, hist, new, tier=0, heads=(4, 2, 128), layers=1, **cfg):
+        hq, hkv, d = heads
+        self.m, self.hist, self.new = m, np.array(hist, np.int32), np.array(new, np.int32)
+        m.device(0)
+        pages = (self.hist + self.new + 15) // 16
+        self.num_pages = int(pages.sum()) + 1
+        self.table = np.full((len(hist), int(pages.max())), -1, np.int32)
+        first = np.concatenate([[0], np.cumsum(pages)])
+        for c in range(len(hist)):
+            self.table[c, :pages[c]] = range(first[c], first[c + 1])
+        total, context = int(self.new.sum()), int((self.hist + self.new).sum())
+        self.ctx = ca.Context(ca.Config(n_layers=layers, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, max_positions=int((self.hist + self.new).max()), max_seqs=len(hist),
+                                        max_batch_kv_tokens=context + 64, max_batch_q_tokens=total + 16, **cfg), kv_bits=4)
+        self.row = self.ctx.kv_row_bytes
+        self.kp, self.vp = (m.alloc(self.num_pages * self.ctx.kv_page_bytes) for _ in range(2))
+        self.tk, self.tv = ([m.alloc(int(r) * self.row, tier) for r in self.hist + self.new] for _ in range(2))
+        self.q, self.out = (m.alloc(total * hq * d * 2) for _ in range(2))
+        self.nk, self.nv = (m.alloc(total * hkv * d * 2) for _ in range(2))
+        self.scale = d ** -0.5
+
+
+# Shares of 33 MiB, which the static call takes only where nothing but the last round of workgroups is cut
+@pytest.mark.parametrize("heads,hist,new", [((64, 4, 64), [3327, 5094, 3895, 2850], [223, 355, 348, 368]),
+                                            ((64, 4, 64), [15489, 6862, 10754, 7958, 14590, 5666], [315, 248, 210, 149, 292, 215]),
+                                            ((32, 4, 64), [6625, 10010, 3869], [1450, 1023, 1182])])
+@in_model
+def test_what_the_static_call_takes_does_not_depend_on_plans_that_were_not_taken(m, heads, hist, new):
+    t = Turn4(m, hist, new, heads=heads, require_load=0, attn_tile_rows=128)
+    t.rebase()
+    taken = t.ctx.rebase_read(6)
+    answers = []
+    for prerotate in (0, 1, 2):                    # both ways, then each for itself
+        one = t if prerotate == 0 else Turn4(m, hist, new, heads=heads, require_load=0, attn_tile_rows=128, attn_prerotate=prerotate)
+        one.rebase()
+        same = np.array_equal(one.ctx.rebase_read(6), taken)
+        try:
+            one.attn(static=True)
+            answers.append((same, "taken"))
+        except ca.CaError as e:
+            answers.append((same, e.status_name))
+    alone = [a for a in answers[1:] if a[0]]
+    assert alone and all(a == (True, "CA_ERR_OUT_OF_RANGE") for a in [answers[0]] + alone), answers

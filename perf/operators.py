@@ -7,7 +7,9 @@ byte a value in the pool and in the tier.  The operators are the ones a serving 
                model does so), and read back as the values that the cache holds from then on
   op "attend"  attention of the new tokens over the context in the pool: decode steps, turns, first turns; the heads of the queries
                are normalised where the model does so, and rotated to their positions, in the same pass
-  op "turn"    all of a turn: rebase, load of the kept history from the tier, append and save, attention
+  op "turn"    all of a turn: load of the kept history from the tier, append and save, attention
+
+Each pass begins with the plan of its batch (positions, work lists), as a step of a serving program does.
 
 Format.  A row is the head_dim values of one token and kv head.  Of every 32 of them, with the largest magnitude M, p is the smallest
 integer from -127 on with M <= 6 * 2^p, the scale byte is p + 127, and a value x becomes the e2m1 number nearest to x / 2^p (0, 0.5, 1,
@@ -229,8 +231,6 @@ def prepare(case: dict, seed: int) -> dict:
         if case["norm"]:
             for l in range(L):
                 ctx.head_norm_set(l, s["q_weight"][l], s["k_weight"][l], EPS)
-        if case["op"] != "turn":
-            ctx.rope_rebase(s["hist"], s["keep_start"], s["new"], s["table"], s["num_pages"])
         if case["op"] != "append":
             s["out"] = torch.zeros_like(s["q"])
         if case["op"] != "attend":
@@ -251,12 +251,13 @@ def run(state: dict):
 def _run_own(s: dict):
     ctx, case, stream = s["ctx"], s["case"], torch.cuda.current_stream()
     layers = range(case["layers"])
+    # the plan of the batch: every step has another one, whatever of the step is measured
+    ctx.rope_rebase(s["hist"], s["keep_start"], s["new"], s["table"], s["num_pages"], stream)
     if case["op"] == "attend":
         for l in layers:
             ctx.cached_prefill_attn(l, s["q"][l], s["k_pool"][l], s["v_pool"][l], s["out"][l], s["scale"], stream)
         return {"out": s["out"]}
     if case["op"] == "turn":
-        ctx.rope_rebase(s["hist"], s["keep_start"], s["new"], s["table"], s["num_pages"], stream)
         for l in layers:
             ctx.kv_load_layer(l, s["at_tier_k"][l], s["at_tier_v"][l], s["k_pool"][l], s["v_pool"][l])
     for l in layers:

@@ -28,8 +28,9 @@ __device__ inline float over_row(float v, F f) {
 //     table of 64 positions in LDS, and the queries once for every such block by what is left.  Both in packed fp16, eleven bits where
 //     bf16 operands have eight: 48 vector instructions a page for the conversion and the rotation of its keys, where advancing
 //     the angles in fp32 and rotating in fp32 take 160.
-//   * The range of fp16: queries are scaled by a power of two to at most 1, the keys of a step by another to at most 6 (the largest scale byte
-//     of the step); the scores are multiplied by both in fp32.
+//   * The range of fp16: queries are scaled by a power of two to at most 1, and where a key of a step leaves the range's middle every key of it
+//     by one of its own to at most 6; the scores are multiplied by both in fp32.  Bits are lost (all of them 2^14 further down) where a
+//     block of a key has less than 2^-10 of 1, or of the key's largest block, and where dimensions of a query have less than 2^-14 of its largest.
 //   * O^T += V^T P^T, 32 keys an instruction, in bf16, which holds codes times scales exactly.  A lane reads 32 codes, the block of one
 //     scale byte, and writes them to LDS as bf16; the transposing reads bring them back as operands.
 //   * The codes and scales of the next step are asked for as soon as this one's are converted, into the same registers.
@@ -245,32 +246,27 @@ __global__ __launch_bounds__(256, 3) void attn_kv4_kernel(AttnArgs a) {
             }
         }
         // ---- keys: rotated operands, one page after the other ----
-        // the largest scale byte of the step's keys (of those that are numbers), over the sixteen lanes of a group
-        uint32_t e_most = 1;
-        uint32_t e_lo[2], e_hi[2];
+        // Where some key's largest scale byte leaves the middle of fp16's range (no value past 6 * 2^12 before its rotation; 2^-10 keeps its bits),
+        // every key of the step is divided by its own: what other keys hold takes no bits from it.
+        uint32_t e_all[2], e_key[2];
+        bool far = false;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const uint32_t e = key0 + x * kPageSize + m16 < kmax ? s.k_e[x] : 0u;
-            const int lo_block = KW == 2 ? q4 >> 1 : 0, hi_block = KW == 2 ? 2 + (q4 >> 1) : 1;
-            e_lo[x] = e >> 8 * lo_block & 255u;
-            e_hi[x] = e >> 8 * hi_block & 255u;
-#pragma unroll
-            for (int b = 0; b < D / 32; ++b) {
-                const uint32_t one = e >> 8 * b & 255u;
-                e_most = max(e_most, kv4_is_nan(one) ? 0u : one);
-            }
+            const bool valid = key0 + x * kPageSize + m16 < kmax;
+            e_all[x] = valid ? s.k_e[x] : 0u;
+            e_key[x] = kv4_most_scale<D>(e_all[x]);
+            far = far || (valid && (e_key[x] < 127 - 10 || e_key[x] > 127 + 12));
         }
-        e_most = max(e_most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)e_most, 0x128, 0xf, 0xf, false));      // row_ror:8, 4, 2, 1
-        e_most = max(e_most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)e_most, 0x124, 0xf, 0xf, false));
-        e_most = max(e_most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)e_most, 0x122, 0xf, 0xf, false));
-        e_most = max(e_most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)e_most, 0x121, 0xf, 0xf, false));
-        const float up = q_up * kv4_scale(e_most);
+        const bool apart = __builtin_amdgcn_ballot_w64(far) != 0;
         f32x4 S[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            // 2^(e - e_most), zero past the range of a float; NaN for NaN
-            const float s_lo = kv4_is_nan(e_lo[x]) ? NAN : kv4_scale((uint32_t)max((int)(e_lo[x] - e_most) + 127, 0));
-            const float s_hi = kv4_is_nan(e_hi[x]) ? NAN : kv4_scale((uint32_t)max((int)(e_hi[x] - e_most) + 127, 0));
+            const int shift = apart ? 127 - (int)e_key[x] : 0;
+            const auto scale_of = [&](int block) CA_INLINE {               // (zero past the range of a float)
+                const uint32_t e = e_all[x] >> 8 * block & 255u;
+                return kv4_scale(kv4_is_nan(e) ? 255u : (uint32_t)max((int)e + shift, 0));
+            };
+            const float s_lo = scale_of(KW == 2 ? q4 >> 1 : 0), s_hi = scale_of(KW == 2 ? 2 + (q4 >> 1) : 1);
             const uint8_t *row = angles + (pair % 2 * 2 * kPageSize + x * kPageSize + m16) * QSTR + q4 * (D / 2);
             uint32_t cw[4 * KW], sw[4 * KW];
 #pragma unroll
@@ -304,8 +300,17 @@ __global__ __launch_bounds__(256, 3) void attn_kv4_kernel(AttnArgs a) {
         }
         // ---- softmax ----
         const float nm = m_run == -INFINITY ? 0.f : -m_run;
+        if (apart) {
+            const int q_exponent = (int)(__float_as_uint(q_up) >> 23) - 127;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) S[i / 4][i % 4] = S[i / 4][i % 4] * up + nm;
+            for (int i = 0; i < 8; ++i) {      // (key 4 q4 + i of a page is that of lane 4 q4 + i in each group)
+                const int k_exponent = __shfl((int)e_key[i / 4], 16 * q4 + 4 * q4 + i % 4) - 127;
+                S[i / 4][i % 4] = __builtin_ldexpf(S[i / 4][i % 4], q_exponent + k_exponent) + nm;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) S[i / 4][i % 4] = S[i / 4][i % 4] * q_up + nm;
+        }
         if (key0 + 2 * kPageSize - 1 > min(n, kmax - 1)) {               // some key of the step may be hidden from some row
 #pragma unroll
             for (int i = 0; i < 8; ++i)

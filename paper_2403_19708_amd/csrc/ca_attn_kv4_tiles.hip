@@ -8,10 +8,12 @@
 // itself, but two of 128 rows with heads of 64 share one (128 registers a thread, which costs a spilled address or none: 221 -> 175 us for
 // 16 first turns of 128-2048 tokens, 32/4 heads).
 //
-// Roundings: rotated queries and keys to fp16, eleven bits, since a key of four bits leaves no range to bf16 that a power of two for eight
-// keys would not hold (convert_keys), nor a query more than one for its row (query_pieces); values not at all (two significant bits);
-// probabilities to bf16, of which the denominator sums what the product uses.  Relative error against 64 bits 0.0022, half of that from the
-// output's own rounding, where operands rotated in fp32 and rounded to bf16 had 0.0033.
+// Roundings: queries rotated in fp32 to fp16, eleven bits; keys rotated in packed fp16 with angles in fp16; values not at all (two significant
+// bits); probabilities to bf16, of which the denominator sums what the product uses.  Relative error against 64 bits 0.0022, half of that
+// from the output's own rounding, where operands rotated in fp32 and rounded to bf16 had 0.0033.  The range of fp16: a power of two for a
+// query row (query_pieces) and one for a key (key_shift) where it leaves the middle.  Bits are lost (all of them 2^14 further down) where a
+// block of 32 dimensions of a key has less than 2^-10 of 1, or of the key's largest block, and where dimensions of a query have less than
+// 2^-14 of the row's largest.
 //
 // What bounds it: a tile of 256 rows is 2176 cycles of matrix instructions a SIMD, 2050 of reads from LDS a compute unit, and some 1900 of
 // vector instructions a SIMD; it takes 2.2 us, some 4600 cycles, and one of 128 rows 1.5, where the kernel over expanded keys
@@ -64,9 +66,10 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
 
     __shared__ __attribute__((aligned(16))) uint8_t smem[2 * (KBUF + VBUF)];
     __shared__ uint64_t v_bad[2][NW];
+    enum : uint8_t { kBad = 1, kShifted = 2 };
     struct Flags {
-        int8_t up[NW];                               // powers of two that the keys of a wavefront were divided by
-        uint8_t bad[NW];                             // some of its values are NaN
+        uint8_t marks[NW];                           // of a wavefront: some of its values are NaN, some of its keys were divided
+        int8_t up[BN];                               // ... by this power of two
     };
     __shared__ __attribute__((aligned(16))) Flags flags[2];
     __shared__ float q_up[32 * GROUPS];              // factors of the rows of the queries
@@ -171,20 +174,15 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
     __syncthreads();
 
     // ---- codes -> fp16 keys and bf16 values in LDS
-    // Keys whose largest scale byte leaves the middle of fp16's range (no value past 6 * 2^12 before its rotation; 2^-10 keeps its bits): those of
-    // the wavefront are divided by the power of two returned.  Asked for in front of the products, whose block a branch would end.
+    // Where a scale byte leaves the middle of fp16's range (no value past 6 * 2^12 before its rotation; 2^-10 keeps its bits), every key of the
+    // wavefront is divided by the power of two returned, its own largest scale: what other keys hold takes no bits from it.  Asked for in front
+    // of the products, whose block a branch would end.
     auto key_shift = [&](uint32_t e, int tile) CA_INLINE {
         const bool valid = tile * BN + row < kmax;
         const int block = sub * E / 32;
         const uint32_t e_lo = e >> 8 * block & 255u, e_hi = e >> (8 * block + D / 8) & 255u, most = max(e_lo, e_hi);
         int up = 0;
-        if (__builtin_amdgcn_ballot_w64(valid && (most > 127 + 12 || most < 127 - 10)) != 0) {
-            int all = max(kv4_is_nan(e_lo) ? 0 : (int)e_lo, kv4_is_nan(e_hi) ? 0 : (int)e_hi);
-            if (!valid) all = 0;
-#pragma unroll
-            for (int m = 1; m < 64; m *= 2) all = max(all, __shfl_xor(all, m));
-            up = __builtin_amdgcn_readfirstlane(all) - 127;
-        }
+        if (__builtin_amdgcn_ballot_w64(valid && (most > 127 + 12 || most < 127 - 10)) != 0 && valid) up = (int)kv4_most_scale<D>(e) - 127;
         return up;
     };
     auto convert_keys = [&](const RawKey &s, int up, int tile) CA_INLINE {
@@ -194,7 +192,7 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
         uint32_t e_lo = s.e >> 8 * block & 255u, e_hi = s.e >> (8 * block + D / 8) & 255u;
         e_lo = !valid ? 0u : kv4_is_nan(e_lo) ? 255u : (uint32_t)max((int)e_lo - up, 0);
         e_hi = !valid ? 0u : kv4_is_nan(e_hi) ? 255u : (uint32_t)max((int)e_hi - up, 0);
-        flags[buf].up[wave] = (int8_t)up;
+        flags[buf].up[row] = (int8_t)up;
         const float s_lo = kv4_scale(e_lo), s_hi = kv4_scale(e_hi);
         uint32_t lo[KW], hi[KW];
 #pragma unroll
@@ -213,12 +211,12 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
             *reinterpret_cast<uint2 *>(to + D) = make_uint2(hi[0], hi[1]);
         }
     };
-    auto convert_values = [&](const RawValue &s, int tile) CA_INLINE {
+    auto convert_values = [&](const RawValue &s, int up, int tile) CA_INLINE {
         const int buf = tile & 1;
         const bool valid = tile * BN + row < kmax, bad = valid && kv4_is_nan(s.e);
         const uint64_t bads = __builtin_amdgcn_ballot_w64(bad);
         v_bad[buf][wave] = bads;               // by all lanes: a branch would end the block that the conversion shares with the products
-        flags[buf].bad[wave] = bads != 0;
+        flags[buf].marks[wave] = (bads != 0 ? kBad : 0) | (__builtin_amdgcn_ballot_w64(up != 0) != 0 ? kShifted : 0);
         const float scale = kv4_scale(valid && !bad ? s.e : 0u);
         uint8_t *const v_to = smem + 2 * KBUF + buf * VBUF + row * VSTR + 16 * VW * sub;
 #pragma unroll
@@ -245,17 +243,18 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
                 S[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8v *>(kb + 32 * mb * KSTR + 32 * ks), Qf[ks], ks == 0 ? neg_ref : S[mb], 0, 0, 0);
     };
     // softmax and second product of `tile`
-    auto multiply = [&](int tile, const u32x4 &flag, bool scaled) CA_INLINE {
+    auto multiply = [&](int tile, const u32x2 &flag, bool scaled) CA_INLINE {
         const int buf = tile & 1, kt0 = tile * BN + 32 * mb0;
-        if (scaled) {                              // from units of the row and of the eight keys of a wavefront
+        if (scaled) {                              // from units of the row and of the key
             const float neg = m_run == -INFINITY ? 0.f : -m_run;
+            const int up = (int)(__float_as_uint(row_up) >> 23) - 127;
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                 for (int i4 = 0; i4 < 4; ++i4) {
-                    const float f = __builtin_ldexpf(row_up, flags[buf].up[4 * (mb0 + mb) + i4]);
+                    const uint32_t ups = *reinterpret_cast<const uint32_t *>(&flags[buf].up[32 * (mb0 + mb) + 8 * i4 + 4 * half]);
 #pragma unroll
-                    for (int i = 4 * i4; i < 4 * i4 + 4; ++i) S[mb][i] = S[mb][i] * f + neg;
+                    for (int i = 0; i < 4; ++i) S[mb][4 * i4 + i] = __builtin_ldexpf(S[mb][4 * i4 + i], up + (int8_t)(ups >> 8 * i)) + neg;
                 }
 #pragma unroll
             for (int i = 0; i < 16; ++i) neg_ref[i] = neg;
@@ -318,7 +317,7 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
             }
         }
         __builtin_amdgcn_s_setprio(0);
-        if (__builtin_amdgcn_readfirstlane(flag[2] | flag[3]) != 0) {       // values that are NaN: the rows that see them
+        if ((__builtin_amdgcn_readfirstlane(flag[0] | flag[1]) & kBad * 0x01010101u) != 0) {       // values that are NaN: the rows that see them
             uint32_t seen = 0;                                       // bit: this lane's row sees one in that block of dimensions
             for (int w = 0; w < NW; ++w)
                 for (uint64_t left = v_bad[buf][w]; left; left &= left - 1) {
@@ -338,13 +337,14 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
     // last page is asked for and converted once more, for nobody.)
     auto ahead = [&](int tile, int up) CA_INLINE {
         convert_keys(raw_k, up, tile + 1);
-        convert_values(raw_v, tile + 1);
+        convert_values(raw_v, up, tile + 1);
         issue_keys(raw_k, page2, tile + 2);
         issue_values(raw_v, page2);
         page2 = page_of(tile + 3);
     };
-    convert_keys(raw_k, key_shift(raw_k.e, t_begin), t_begin);
-    convert_values(raw_v, t_begin);
+    const int up0 = key_shift(raw_k.e, t_begin);
+    convert_keys(raw_k, up0, t_begin);
+    convert_values(raw_v, up0, t_begin);
     issue_keys(raw_k, page1, t_begin + 1);
     issue_values(raw_v, page1);
     __syncthreads();
@@ -352,8 +352,8 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
     int tile = t_begin;
     for (; tile < n_mine; ++tile) {
         const int up = key_shift(raw_k.e, tile + 1);
-        const u32x4 flag = *reinterpret_cast<const u32x4 *>(&flags[tile & 1]);
-        const bool scaled = rows_scaled || __builtin_amdgcn_readfirstlane(flag[0] | flag[1]) != 0;
+        const u32x2 flag = *reinterpret_cast<const u32x2 *>(flags[tile & 1].marks);
+        const bool scaled = rows_scaled || (__builtin_amdgcn_readfirstlane(flag[0] | flag[1]) & kShifted * 0x01010101u) != 0;
         if (scaled) neg_ref = f32x16{};            // (the reference would be of other units)
         scores(tile);
         ahead(tile, up);

@@ -26,7 +26,17 @@ struct Kv4 {
 
 __device__ inline bool kv4_is_nan(uint32_t e) { return e > kKv4MostScale; }
 __device__ inline float kv4_scale(uint32_t e) { return __uint_as_float(e << 23); }      // as the conversions take it (0: 2^-127)
-
+// the largest of a key's scale bytes that are numbers
+template <int D>
+__device__ __attribute__((always_inline)) inline uint32_t kv4_most_scale(uint32_t e) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) {
+        const uint32_t one = e >> 8 * b & 255u;
+        most = max(most, kv4_is_nan(one) ? 0u : one);
+    }
+    return most;
+}
 
 // codes of a word -> values 2 i and 2 i + 1
 __device__ __attribute__((always_inline)) inline float2 pair_f32(uint32_t w, float scale, int i) {

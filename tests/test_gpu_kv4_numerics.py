@@ -1,0 +1,95 @@
+"""Attention over the 4-bit cache on the GPU, held closer than a worst case allows, by the mean square of its error against 64 bits: keys of very
+different sizes side by side."""
+import numpy as np
+import pytest
+import torch
+
+import kv4_oracle as o4
+from synth import bf16_bits_to_f64, draw_values_bf16
+from test_gpu_kv4 import Turn, to_bits, to_torch, turn  # noqa: F401 (the fixture)
+
+pytestmark = pytest.mark.gpu
+
+# path: the switches that choose it, most rows a unit may have there, roundings of the operands of the score product (in units of the root mean
+# square of one, for the root of their sum), and of the probabilities and the output
+ROWS, TILES128, TILES256, EXPANDED, SCALAR = "few rows", "tiles of 128", "tiles of 256", "expanded", "scalar"
+SWITCHES = {ROWS: dict(), TILES128: dict(attn_prerotate=1, attn_tile_rows=128), TILES256: dict(attn_prerotate=1, attn_tile_rows=256), EXPANDED: dict(attn_prerotate=2),
+            SCALAR: dict(attn_variant=1)}
+# Relative root mean square of a rounding to s significant bits: the error is uniform up to half a step, 2^-s of the power of two below the
+# value, and mantissas m are spread like their logarithm: 2^-s / sqrt(3) * sqrt(mean of 1 / m^2) = 2^-s * 0.425.
+U8, U11 = 2.0 ** -8 * 0.425, 2.0 ** -11 * 0.425
+# Of a rotation in fp16 the angle, a product and the sum are rounded, and the part of the pair that is left out of a component is no larger than
+# the pair: 3 roundings, of up to sqrt(2) of the component.  Queries are rounded before they are rotated (few rows), or behind (tiles), keys not.
+OPERANDS = {ROWS: 2 ** 0.5 * 7 ** 0.5 * U11, TILES128: 2 ** 0.5 * 4 ** 0.5 * U11, TILES256: 2 ** 0.5 * 4 ** 0.5 * U11, EXPANDED: 2 ** 0.5 * U8, SCALAR: 0.0}
+PROBABILITIES = {ROWS: U8, TILES128: U8, TILES256: U8, EXPANDED: U8, SCALAR: 0.0}
+
+
+def exact(t, c, g):
+    """outputs of the heads of kv head g of conversation c, and the root mean square of the size that score errors scale with"""
+    G, mine = t.Hq // t.H, slice(t.cu[c], t.cu[c + 1])
+    q = bf16_bits_to_f64(t.q[mine, g * G:(g + 1) * G])
+    if t.qw is not None:
+        q = o4.head_norm(q, t.qw, t.eps)
+    k, v = t.context(0, c)[:, g], t.context(1, c)[:, g]
+    n = int(t.n[c])
+    qr, kr = o4.rotate(q, n + np.arange(len(q)), t.style), o4.rotate(k[:, None], np.arange(len(k)), t.style)[:, 0]
+    s = np.einsum("jhd,td->jht", qr, kr) * t.scale
+    size = np.einsum("jhd,td->jht", qr * qr, kr * kr) * t.scale ** 2
+    hidden = np.arange(len(k))[None] > (n + np.arange(len(q)))[:, None]
+    s = np.where(hidden[:, None], -np.inf, s)
+    p = np.exp(s - s.max(-1, keepdims=True))
+    p /= p.sum(-1, keepdims=True)
+    return p @ v, float((p * size).sum(-1).mean())
+
+
+def check_rms(t, path, slack=1.25):
+    """Root mean square of the error over that of the outputs.  Output and probabilities are rounded to 8 bits; a score off by d moves the output by
+    its probability times d (v - out), no more than the output's own size times d where values have no common part.  The slack is for
+    how far a mean over few rows may be off (a hundred roundings: 7 %), and for values with one."""
+    got = bf16_bits_to_f64(to_bits(t.out))
+    G = t.Hq // t.H
+    err = size = 0.0
+    score = []
+    for c in range(t.B):
+        for g in range(t.H):
+            want, s = exact(t, c, g)
+            score.append(s * len(want))
+            err += ((got[t.cu[c]:t.cu[c + 1], g * G:(g + 1) * G] - want) ** 2).sum()
+            size += (want ** 2).sum()
+    s2 = sum(score) / (t.H * t.cu[-1])
+    limit = slack * np.sqrt(U8 ** 2 + PROBABILITIES[path] ** 2 + OPERANDS[path] ** 2 * s2)
+    assert np.sqrt(err / size) <= limit, (np.sqrt(err / size), limit, np.sqrt(s2))
+
+
+def run(t):
+    t.rebase()
+    t.load()
+    t.append()
+    t.attend()
+    t.finish()
+
+
+# ---- keys of very different sizes side by side -------------------------------------------------------------------------------------------
+LOW = 8          # rotary pairs of the lowest frequencies, which a few hundred positions hardly turn
+
+
+@pytest.mark.parametrize("where", ["hidden", "outweighed"])
+@pytest.mark.parametrize("exponent", [18, 20, 24, 40, 100])
+@pytest.mark.parametrize("path,T,Hq,H,D", [(ROWS, 8, 4, 2, 128), (ROWS, 16, 2, 2, 64), (TILES128, 90, 4, 2, 128), (TILES128, 90, 2, 2, 64), (TILES256, 150, 4, 2, 128),
+                                          (TILES256, 150, 2, 2, 64), (EXPANDED, 90, 4, 2, 128), (SCALAR, 20, 2, 2, 64)])
+def test_a_large_key_takes_no_bits_from_the_others(turn, path, T, Hq, H, D, exponent, where):
+    """hidden: the last token's key, which only its own row sees; outweighed: one in the middle whose scores are far below the others'"""
+    f = lambda x: (np.asarray(x, np.float32).view(np.uint32) >> 16).astype(np.uint16)
+    k = bf16_bits_to_f64(draw_values_bf16((T, H, D), 8, 2))
+    q = bf16_bits_to_f64(draw_values_bf16((T, Hq, D), 8, 1))
+    low = np.concatenate([np.arange(D // 2 - LOW, D // 2), np.arange(D - LOW, D)])
+    q[..., low] = 3.0
+    at = T - 1 if where == "hidden" else T // 2
+    k[at] = 0.0
+    k[at, :, low] = -2.0 ** exponent
+    t = turn([0], [T], Hq, H, D, k_new=f(k), seed=8, window=512, **SWITCHES[path])
+    t.q = f(q)
+    t.dq.copy_(to_torch(t.q))
+    run(t)
+    t.check_pools()
+    check_rms(t, path)

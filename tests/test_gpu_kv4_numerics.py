@@ -1,5 +1,5 @@
-"""Attention over the 4-bit cache on the GPU, held closer than a worst case allows, by the mean square of its error against 64 bits: keys of very
-different sizes side by side."""
+"""Attention over the 4-bit cache on the GPU, held closer than a worst case allows: the mean square of its error against 64 bits on every path,
+every key counted exactly once, keys and queries of very different sizes side by side."""
 import numpy as np
 import pytest
 import torch
@@ -67,6 +67,55 @@ def run(t):
     t.append()
     t.attend()
     t.finish()
+
+
+# ---- every path's error ---------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("q_scale", [1.0, 4.0])
+@pytest.mark.parametrize("style,norm", [(0, True), (1, False)])
+@pytest.mark.parametrize("path,hist,new,Hq,H,D", [
+    (ROWS, [700, 40, 301], [1, 4, 2], 16, 4, 128), (ROWS, [500, 3, 129], [5, 16, 1], 4, 4, 64),
+    (TILES128, [300, 0], [90, 140], 4, 2, 128), (TILES128, [300, 0], [90, 140], 3, 3, 64),
+    (TILES256, [200, 60], [150, 33], 4, 2, 128), (TILES256, [200, 60], [150, 33], 4, 4, 64),
+    (EXPANDED, [200, 60], [150, 33], 4, 2, 128), (EXPANDED, [300, 0], [90, 140], 3, 3, 64),
+    (SCALAR, [100, 0], [20, 31], 4, 2, 128), (SCALAR, [100, 0], [20, 31], 2, 2, 64)])
+def test_mean_square_of_the_error(turn, path, hist, new, Hq, H, D, style, norm, q_scale):
+    t = turn(hist, new, Hq, H, D, style=style, norm=norm, q_scale=q_scale, seed=3, **SWITCHES[path])
+    run(t)
+    check_rms(t, path)
+
+
+# ---- every key counts once --------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("marks", ["step", "place"])
+@pytest.mark.parametrize("path,hist,new,Hq,H,D", [
+    (ROWS, [1990, 700, 33], [1, 3, 2], 8, 2, 128), (ROWS, [1200, 64, 1], [2, 1, 16], 2, 2, 64), (ROWS, [1999], [1], 1, 1, 128),
+    (TILES128, [1000, 31], [130, 70], 4, 1, 128), (TILES128, [1300, 31], [130, 70], 2, 2, 64), (TILES256, [1500, 100], [300, 1], 2, 2, 128),
+    (TILES256, [900, 100], [70, 300], 4, 1, 64), (EXPANDED, [1500, 100], [300, 70], 2, 1, 128), (EXPANDED, [900, 3], [300, 20], 4, 2, 64)])
+def test_every_key_counts_once(turn, path, hist, new, Hq, H, D, marks):
+    """Queries of zeros give every visible key the same weight, exactly.  The values of a step of 32 keys are ones in a dimension of the step's
+    own (or those of the same place in a step in the place's own), so that the output is how many of them were counted: one key more or less is a
+    32nd (or one in at most 72) of that, the output's rounding a 256th."""
+    T = sum(new)
+    def ones(tokens, first):
+        at = np.arange(first, first + tokens)
+        v = np.zeros((tokens, H, D), np.uint16)
+        v[np.arange(tokens), :, at // 32 % D if marks == "step" else at % 32] = 0x3F80
+        return v
+    cu = np.concatenate([[0], np.cumsum(new)])
+    v_new = np.concatenate([ones(m, h) for h, m in zip(hist, new)])
+    t = turn(hist, new, Hq, H, D, v_new=v_new, seed=5, **SWITCHES[path])
+    t.q = np.zeros_like(t.q)
+    t.dq.zero_()
+    for c, h in enumerate(hist):
+        t.saved[c][1] = o4.quantise(ones(h, 0))
+        t.tier[1][c][:h] = torch.from_numpy(o4.rows(*t.saved[c][1])).to(t.tier[1][c].device)
+    torch.cuda.synchronize()
+    run(t)
+    got = bf16_bits_to_f64(to_bits(t.out))
+    for c, h in enumerate(hist):
+        v = o4.values(*o4.quantise(ones(h + new[c], 0)))[:, 0]
+        counts = np.cumsum(v, 0)[h:] / (h + 1 + np.arange(new[c]))[:, None]
+        err = np.abs(got[cu[c]:cu[c + 1]] - counts[:, None])
+        assert (err <= counts[:, None] * (2.0 ** -8 + 1e-6)).all(), (c, np.unravel_index(err.argmax(), err.shape))
 
 
 # ---- keys of very different sizes side by side -------------------------------------------------------------------------------------------

@@ -145,10 +145,7 @@ __global__ __launch_bounds__(256, 3) void attn_kv4_kernel(AttnArgs a) {
             u[2 * i + 1] = bf_hi(w[i]);
         }
         if (a.q_weight) {
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += u[i] * u[i];
-            const float inv = rsqrtf(group_sum<PPR>(sum) * (1.0f / D) + a.norm_eps);
+            const float inv = head_norm<D, PPR>(u, a.norm_eps);
             const uint4 gain = *reinterpret_cast<const uint4 *>(a.q_weight + 8 * piece);
             const uint32_t gw[4] = {gain.x, gain.y, gain.z, gain.w};
 #pragma unroll
@@ -561,7 +558,7 @@ __global__ __launch_bounds__(256) void kv4_mark_kernel(AttnArgs a) {
 }
 
 // ---- scalar check kernel ----------------------------------------------------------------------------------------------------------
-// The same operation the slow way, in fp32 throughout and without matrix cores, one wavefront per (new token, query head), a lane per key.
+// The same operation the slow way, in fp32 (the norm in 64 bits) and without matrix cores, one wavefront per (new token, query head), a lane per key.
 template <int D>
 __global__ __launch_bounds__(64) void attn_kv4_ref_kernel(AttnArgs a) {
     constexpr int HALF = D / 2;
@@ -580,18 +577,18 @@ __global__ __launch_bounds__(64) void attn_kv4_ref_kernel(AttnArgs a) {
     __shared__ float qr[D];
     {
         const uint16_t *q = a.q + ((int64_t)i * a.n_q_heads + h) * D;
-        float inv = 1.f;
+        double inv = 1.0;
         if (a.q_weight) {
-            float sum = 0.f;
-            for (int d = lane; d < D; d += 64) sum += bf_lo(q[d]) * bf_lo(q[d]);
+            double sum = 0.0;
+            for (int d = lane; d < D; d += 64) sum += (double)bf_lo(q[d]) * (double)bf_lo(q[d]);
             for (int w = 32; w >= 1; w >>= 1) sum += __shfl_xor(sum, w);
-            inv = 1.0f / sqrtf(sum * (1.0f / D) + a.norm_eps);
+            inv = 1.0 / sqrt(sum / D + (double)a.norm_eps);
         }
         for (int p = lane; p < HALF; p += 64) {
             const int ia = first(p), ib = second(p);
             const float2 cs = a.rope[(int64_t)pos * HALF + p];
             float x = bf_lo(q[ia]), y = bf_lo(q[ib]);
-            if (a.q_weight) { x *= inv * bf_lo(a.q_weight[ia]); y *= inv * bf_lo(a.q_weight[ib]); }
+            if (a.q_weight) { x = (float)(x * inv * bf_lo(a.q_weight[ia])); y = (float)(y * inv * bf_lo(a.q_weight[ib])); }
             qr[ia] = x * cs.x - y * cs.y;
             qr[ib] = y * cs.x + x * cs.y;
         }

@@ -154,6 +154,39 @@ __device__ __attribute__((always_inline)) inline float group_sum(float x) {
     return x;
 }
 
+// 1 / sqrt(mean(x^2) + eps) of a head of D values, N of them in each of LANES neighbouring lanes, all active.  In fp32; rows whose mean is past
+// its range on either side (of values above 2^60, or below 2^-50 with an eps of zero) are first divided by the power of two of their largest.
+template <int D, int LANES, int N>
+__device__ __attribute__((always_inline)) inline float head_norm(float (&x)[N], float eps) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum += x[i] * x[i];
+    float mean = group_sum<LANES>(sum) * (1.0f / D) + eps;
+    const bool past = !(mean >= 0x1p-100f && mean < INFINITY);
+    if (__builtin_amdgcn_ballot_w64(past) != 0) {
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(x[i]));
+#pragma unroll
+        for (int m = 1; m < LANES; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+        const int e = (int)(__float_as_uint(most) >> 23) - 126;
+        float y[N];
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            y[i] = __builtin_ldexpf(x[i], -e);
+            sum += y[i] * y[i];
+        }
+        const float scaled = group_sum<LANES>(sum) * (1.0f / D) + __builtin_ldexpf(eps, -2 * e);
+        if (past) {
+            mean = scaled;
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = y[i];
+        }
+    }
+    return rsqrtf(mean);
+}
+
 // The 32 stacked query rows row_first .. of a wavefront, rotated, scaled by `f` and rounded, as B operand of S^T = K Q^T (lane ->
 // row lane % 32, k-step ks -> piece 2 ks + lane / 32).  A lane that fetches its own row touches 32 cache lines in every
 // instruction, each line in four instructions, for the queries and again for the rotary table, and the first level cache does not hold
@@ -207,9 +240,9 @@ struct QueryRows {
             const float2 first = make_float2(cs[i].x, cs[i].y), second = make_float2(cs[i].z, cs[i].w);
             const float2 both[8] = {first, second, first, second, second, second, second, second};
             if (NORM) {
-                const float a0 = bf_lo(x[i]), a1 = bf_hi(x[i]), b0 = bf_lo(y[i]), b1 = bf_hi(y[i]);
-                const float inv = f * rsqrtf(group_sum<LPR>(a0 * a0 + a1 * a1 + b0 * b0 + b1 * b1) * (1.0f / D) + eps);
-                const float u0 = a0 * inv * gain[0], u1 = a1 * inv * gain[1], v0 = b0 * inv * gain[2], v1 = b1 * inv * gain[3];
+                float of[4] = {bf_lo(x[i]), bf_hi(x[i]), bf_lo(y[i]), bf_hi(y[i])};
+                const float inv = f * head_norm<D, LPR>(of, eps);
+                const float u0 = of[0] * inv * gain[0], u1 = of[1] * inv * gain[1], v0 = of[2] * inv * gain[2], v1 = of[3] * inv * gain[3];
                 if (STYLE == 0) {                                // pairs (u0, v0), (u1, v1)
                     x[i] = pack_bf16(u0 * first.x - v0 * first.y, u1 * second.x - v1 * second.y);
                     y[i] = pack_bf16(v0 * first.x + u0 * first.y, v1 * second.x + u1 * second.y);

@@ -103,17 +103,15 @@ __device__ __attribute__((always_inline)) inline float query_pieces(const AttnAr
     float2 cs[8];
     load_cs<D, STYLE>(a.rope, pos, piece, cs);
     uint32_t *px = reinterpret_cast<uint32_t *>(&x), *py = reinterpret_cast<uint32_t *>(&y);
-    float u[8], v[8];
+    float of[16];                                        // eight of either half
+    float *const u = of, *const v = of + 8;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         u[2 * w] = bf_lo(px[w]); u[2 * w + 1] = bf_hi(px[w]);
         v[2 * w] = bf_lo(py[w]); v[2 * w + 1] = bf_hi(py[w]);
     }
     if (a.q_weight) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += u[i] * u[i] + v[i] * v[i];
-        const float inv = rsqrtf(group_sum<D / 16>(sum) * (1.0f / D) + a.norm_eps);
+        const float inv = head_norm<D, D / 16>(of, a.norm_eps);
         const uint4 gx = *reinterpret_cast<const uint4 *>(a.q_weight + 8 * piece), gy = *reinterpret_cast<const uint4 *>(a.q_weight + HALF + 8 * piece);
         const uint32_t *wx = reinterpret_cast<const uint32_t *>(&gx), *wy = reinterpret_cast<const uint32_t *>(&gy);
 #pragma unroll

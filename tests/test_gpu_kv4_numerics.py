@@ -142,3 +142,23 @@ def test_a_large_key_takes_no_bits_from_the_others(turn, path, T, Hq, H, D, expo
     run(t)
     t.check_pools()
     check_rms(t, path)
+
+
+# ---- norms of queries and keys whose squares are past the range of 32 bits ------------------------------------------------------------------
+@pytest.mark.parametrize("eps", [1e-6, 0.0])
+@pytest.mark.parametrize("exponent", [120, 70, -60, -70, -125, "mixed"])
+@pytest.mark.parametrize("path,T,Hq,H,D", [(ROWS, 8, 4, 2, 128), (ROWS, 16, 2, 2, 64), (TILES128, 90, 4, 2, 128), (TILES256, 150, 2, 2, 64), (EXPANDED, 90, 4, 2, 128),
+                                          (EXPANDED, 90, 2, 2, 64), (SCALAR, 20, 4, 2, 128)])
+def test_norms_of_heads_of_any_size(turn, path, T, Hq, H, D, exponent, eps):
+    f = lambda x: (np.asarray(x, np.float32).view(np.uint32) >> 16).astype(np.uint16)
+    sizes = 2.0 ** (np.array([0, 100, -70, 64, -10, -124])[np.arange(T) % 6] if exponent == "mixed" else np.full(T, float(exponent)))
+    k = f(bf16_bits_to_f64(draw_values_bf16((T, H, D), 8, 2)) * sizes[:, None, None])
+    t = turn([0], [T], Hq, H, D, k_new=k, seed=8, norm=True, style=T % 4 // 2, window=512, **SWITCHES[path])
+    t.eps = eps
+    t.ctx.head_norm_set(0, *t.weights, eps)
+    t.appended[0] = o4.quantise(o4.f64_to_bf16_bits(o4.head_norm(bf16_bits_to_f64(k), t.kw, eps)))
+    t.q = f(bf16_bits_to_f64(draw_values_bf16((T, Hq, D), 8, 1)) * sizes[:, None, None])
+    t.dq.copy_(to_torch(t.q))
+    run(t)
+    t.check_pools()
+    check_rms(t, path)

@@ -85,7 +85,7 @@ struct Kv4Append {
     double eps;
     int32_t first_token, end_token, first_seq, max_pages, n_kv_heads, row_bytes;
 };
-hipError_t launch_kv4_append(const Kv4Append &args, int head_dim, bool save, hipStream_t stream);
+hipError_t launch_kv4_append(const Kv4Append &args, int head_dim, bool save, int n_cus, hipStream_t stream);
 // launch_move / launch_link for it (workgroups 0: as many as there is work for), and context tokens -> bf16 rows
 hipError_t launch_kv4_move(bool to_pool, const MoveArgs &args, const MoveShape &shape, int head_dim, int row_bytes, int workgroups, uint8_t *k_pool,
                            uint8_t *v_pool, hipStream_t stream);

@@ -217,14 +217,14 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(MoveArgs a, MoveShap
 
 }  // namespace
 
-hipError_t launch_kv4_append(const Kv4Append &a, int head_dim, bool save, hipStream_t stream) {
+hipError_t launch_kv4_append(const Kv4Append &a, int head_dim, bool save, int n_cus, hipStream_t stream) {
     const int n = a.end_token - a.first_token;
     if (n <= 0) return hipSuccess;
     const int tokens = kThreads / (head_dim / 8);
     // a head per thread until every compute unit has 16 workgroups of that: the loads of more need fewer wavefronts, and a token's table
     // entries are looked up once
     const int64_t groups = (n + tokens - 1) / tokens;
-    const int heads = 2 * groups * a.n_kv_heads > 16 * 256 ? 4 : 1;
+    const int heads = 2 * groups * a.n_kv_heads > (int64_t)16 * n_cus ? 4 : 1;
     const dim3 grid((uint32_t)groups * (uint32_t)((a.n_kv_heads + heads - 1) / heads), 2);
     if (head_dim != 128 && head_dim != 64) return hipErrorInvalidValue;
     const auto kernel = head_dim == 128 ? (save ? (heads == 4 ? kv4_append_kernel<128, true, 4> : kv4_append_kernel<128, true, 1>)

@@ -2031,7 +2031,7 @@ ca_status run_append(ca_ctx *ctx, int32_t layer, const void *new_k, const void *
     int iv;
     CA_HIP(ctx, prof_begin(ctx, kProfAppend, stream, &iv));
     if (ctx->kv4) {
-        CA_HIP(ctx, launch_kv4_append(kv4_new_turn(ctx, layer, 0, ctx->n_seqs, new_k, new_v, k_pool, v_pool), ctx->cfg.head_dim, false, stream));
+        CA_HIP(ctx, launch_kv4_append(kv4_new_turn(ctx, layer, 0, ctx->n_seqs, new_k, new_v, k_pool, v_pool), ctx->cfg.head_dim, false, ctx->n_cus, stream));
         CA_HIP(ctx, prof_end(ctx, iv, stream));
         return CA_OK;
     }
@@ -2451,7 +2451,7 @@ ca_status ca_kv_append_save_layer(ca_ctx *ctx, int32_t layer, const void *new_k,
         if (ctx->kv4) {
             Kv4Append a = kv4_new_turn(ctx, layer, at, n, new_k, new_v, k_pool, v_pool);
             a.second = second;
-            CA_HIP(ctx, launch_kv4_append(a, c.head_dim, true, stream));
+            CA_HIP(ctx, launch_kv4_append(a, c.head_dim, true, ctx->n_cus, stream));
             continue;
         }
         CA_HIP(ctx, launch_append_save(new_turn_shape(ctx, at, n), at, second, (const uint8_t *)new_k, (const uint8_t *)new_v,

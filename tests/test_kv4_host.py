@@ -103,6 +103,18 @@ class Turn4(Turn):
         self.scale = d ** -0.5
 
 
+# Four heads to a thread where one would give every compute unit more than 16 workgroups: here 1200 of them
+@pytest.mark.parametrize("cus,heads_to_a_thread", [(256, 1), (80, 1), (64, 4)])
+@in_model
+def test_an_append_is_spread_over_the_compute_units_there_are(m, cus, heads_to_a_thread):
+    m.lib.model_cus(cus)
+    t = Turn4(m, [0], [1200], heads=(8, 8, 128))
+    t.rebase()
+    op, = m.queued(t.append)
+    assert f"kv4_append_kernelILi128ELb0ELi{heads_to_a_thread}E" in m.what(op)
+    assert m.lib.model_workgroups(op) == 75 * 8 // heads_to_a_thread
+
+
 # Shares of 33 MiB, which the static call takes only where nothing but the last round of workgroups is cut
 @pytest.mark.parametrize("heads,hist,new", [((64, 4, 64), [3327, 5094, 3895, 2850], [223, 355, 348, 368]),
                                             ((64, 4, 64), [15489, 6862, 10754, 7958, 14590, 5666], [315, 248, 210, 149, 292, 215]),

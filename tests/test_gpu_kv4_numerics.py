@@ -118,6 +118,55 @@ def test_every_key_counts_once(turn, path, hist, new, Hq, H, D, marks):
         assert (err <= counts[:, None] * (2.0 ** -8 + 1e-6)).all(), (c, np.unravel_index(err.argmax(), err.shape))
 
 
+# ---- batches as they come ----------------------------------------------------------------------------------------------------------------
+HEADS = ((8, 8, 128), (5, 5, 128), (16, 2, 128), (8, 2, 128), (4, 4, 64), (12, 4, 64), (16, 2, 64), (33, 11, 64))
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_batches(turn, seed):
+    """whole turns of decode steps, short and long turns and first turns in any mixture, truncated, by the plan the library chooses"""
+    rng = np.random.default_rng([seed, 41])
+    Hq, H, D = HEADS[seed % len(HEADS)]
+    B = int(rng.integers(1, 7))
+    hist = np.where(rng.random(B) < 0.2, 0, np.exp(rng.uniform(0, np.log(1500), B)).astype(int))
+    new = np.where(rng.random(B) < 0.4, 1, np.exp(rng.uniform(0, np.log(250), B)).astype(int))
+    if seed % 3 == 0:
+        new = np.minimum(new, 4)                                     # a batch of decode steps
+    keep = (hist * rng.random(B) * (rng.random(B) < 0.4)).astype(int)
+    t = turn(hist, new, Hq, H, D, keep=keep, style=int(rng.integers(2)), norm=bool(rng.integers(2)), seed=seed, tier=("device", "pinned")[int(rng.integers(2))],
+             load_mode=int(rng.integers(3)), save_mode=int(rng.integers(3)))
+    t.rebase()
+    t.load()
+    t.append_save()
+    t.attend()
+    t.finish()
+    t.check_pools()
+    t.check_tiers()
+    check_rms(t, EXPANDED)                                           # the loosest of the limits
+    t.out.fill_(float("nan"))
+    before = t.out.clone()
+    t.attend(out=before)
+    t.attend()
+    t.finish()
+    assert torch.equal(before, t.out)
+
+
+@pytest.mark.parametrize("path", [ROWS, TILES128, TILES256, EXPANDED, SCALAR])
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_behind_the_last_sequence_stay_on_every_path(turn, path, D):
+    t = turn([40, 10], [3, 4 if path == ROWS else 70], 4, 2, D, **SWITCHES[path])
+    T = int(t.cu[-1])
+    out = torch.full((T + 4, 4, D), 3.0, dtype=torch.bfloat16, device=t.out.device)
+    t.rebase()
+    t.load()
+    t.append()
+    t.attend(out=out[2:T + 2])
+    t.finish()
+    assert (out[:2] == 3.0).all() and (out[T + 2:] == 3.0).all()
+    t.out.copy_(out[2:T + 2])
+    check_rms(t, path)
+
+
 # ---- keys of very different sizes side by side -------------------------------------------------------------------------------------------
 LOW = 8          # rotary pairs of the lowest frequencies, which a few hundred positions hardly turn
 

@@ -136,3 +136,86 @@ def test_what_the_static_call_takes_does_not_depend_on_plans_that_were_not_taken
             answers.append((same, e.status_name))
     alone = [a for a in answers[1:] if a[0]]
     assert alone and all(a == (True, "CA_ERR_OUT_OF_RANGE") for a in [answers[0]] + alone), answers
+
+
+@pytest.mark.parametrize("load_mode", [0, 1])
+@pytest.mark.parametrize("tier", [0, 1], ids=["device", "pinned"])
+@in_model
+def test_a_whole_turn_waits_for_what_it_reads(m, tier, load_mode):
+    t = Turn4(m, [4000, 30], [200, 1], tier=tier, load_mode=load_mode)
+    s, other = m.stream(), m.stream()
+    ops = m.queued(lambda: (t.rebase(s), t.load(), t.append(s), t.attn(s), t.save(s)))
+    load, save = m.named(ops, "kv4_move_kernel")
+    append, = m.named(ops, "kv4_append_kernel")
+    assert all(m.behind(load, op) for op in m.named(ops, "copy")) and len(m.named(ops, "copy")) == 4 * load_mode
+    attn = m.named(ops, "attn_kv4") + m.named(ops, "attn_prerot") + m.named(ops, "kv4_expand") + m.named(ops, "kv4_mark")
+    assert attn and all(m.behind(op, load) and m.behind(op, append) for op in attn) and m.behind(save, append) and m.behind(save, load)
+    t.ctx.join(other)
+    assert m.stream_behind(other, load) and m.stream_behind(other, save)
+    t.ctx.sync()
+    assert m.done(load) and m.done(save)
+
+
+@pytest.mark.parametrize("new", [[5, 40], [2, 9000]], ids=["short", "long"])
+@pytest.mark.parametrize("tier", [0, 1], ids=["device", "pinned"])
+@in_model
+def test_a_staged_write_back_copies_what_was_packed(m, tier, new):
+    """new_k and new_v are not what the tier holds: the codes are packed from the pools first"""
+    t = Turn4(m, [33, 0], new, tier=tier, save_mode=1, pipeline_depth=2)
+    s, other = m.stream(), m.stream()
+    t.rebase(s)
+    for _ in range(3):                                    # (the third takes the first one's slot)
+        ops = m.queued(lambda: t.append_save(s))
+        append, = m.named(ops, "kv4_append_kernel")
+        pack, = m.named(ops, "kv4_move_kernel")
+        copies = m.named(ops, "copy")
+        assert len(copies) == 4 and m.behind(pack, append) and all(m.behind(op, pack) for op in copies)
+    t.ctx.join(other)
+    assert all(m.stream_behind(other, op) for op in copies)
+    t.ctx.sync()
+    assert all(m.done(op) for op in copies)
+
+
+@pytest.mark.parametrize("tier,mode", [(0, 0), (1, 2), (1, 0)], ids=["device", "pinned-mode2", "pinned"])
+@pytest.mark.parametrize("new", [2, 20000], ids=["short", "long"])
+@in_model
+def test_sync_and_join_cover_append_save(m, new, tier, mode):
+    t = Turn4(m, [0], [new], tier=tier, save_mode=mode)
+    s, s2, other = m.stream(), m.stream(), m.stream()
+    t.rebase(s)
+    saves = [m.queued(lambda: t.append_save(x))[-1] for x in (s, s, s2)]        # (the third while the others are under way)
+    t.ctx.join(other)
+    assert all(m.stream_behind(other, op) for op in saves)
+    t.ctx.sync()
+    assert all(m.done(op) for op in saves)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@in_model
+def test_a_step_can_be_captured(m, new):
+    t = Turn4(m, [100], [new], require_load=0)
+    s, s2 = m.stream(), m.stream()
+    got = [m.alloc(new * t.ctx.cfg.n_kv_heads * t.ctx.cfg.head_dim * 2) for _ in range(2)]
+    t.rebase(s)
+    t.append_save(s2)
+    m.lib.model_capture(s, 1)
+    m.queued(lambda: (t.append_save(s), t.attn(s), t.ctx.kv_read_layer(0, t.kp, t.vp, *got, stream=s)))
+    assert m.lib.model_capture(s, 0)
+    t.ctx.join(s2)
+    t.ctx.sync()
+    t.rebase(s)
+
+
+@in_model
+def test_scratch_copies_are_for_plans_that_may_expand(m):
+    """two bf16 copies of a batch's context and their marks; a context that never expands has none"""
+    def bytes_of(**cfg):
+        before = m.lib.model_device_bytes()
+        t = Turn4(m, [4000], [200], heads=(8, 8, 128), **cfg)
+        made = m.lib.model_device_bytes() - before
+        t.ctx.close()
+        return made
+    bytes_of()                                      # (the first context finds the library's static memory)
+    copies = bytes_of() - bytes_of(attn_prerotate=1)
+    context = (4200 + 64) * 8 * 128 * 2
+    assert 2 * context <= copies <= 2.1 * context

@@ -167,6 +167,47 @@ def test_rows_behind_the_last_sequence_stay_on_every_path(turn, path, D):
     check_rms(t, path)
 
 
+@pytest.mark.parametrize("path,hist,new", [(ROWS, [700, 40, 301], [1, 4, 2]), (TILES128, [300, 0, 9], [90, 140, 1]), (TILES256, [200, 60, 3], [150, 33, 1]),
+                                           (EXPANDED, [200, 60, 0], [150, 33, 1]), (SCALAR, [100, 0, 5], [20, 31, 1])])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("tier", ["device", "pinned"])
+@pytest.mark.parametrize("offset", [2, 5])
+def test_memory_of_any_alignment(turn, path, hist, new, D, tier, offset):
+    """queries, outputs, new keys and values aligned to their elements, pools and tiers to bytes"""
+    t = turn(hist, new, 8, 2, D, seed=6, tier=tier, norm=True, **SWITCHES[path])
+
+    def elsewhere(x, by, pin=False):
+        flat = x.contiguous().reshape(-1).view(torch.uint8)
+        room = torch.zeros(flat.numel() + 64, dtype=torch.uint8, device=x.device)
+        room = room.pin_memory() if pin else room
+        room[by:by + flat.numel()] = flat
+        return room
+    rooms = [elsewhere(x, 2) for x in (t.dq, t.dk, t.dv, t.out)]
+    q, k, v, out = (r.data_ptr() + 2 for r in rooms)
+    pool_rooms = [elsewhere(x, offset) for x in t.pools]
+    pools = [r.data_ptr() + offset for r in pool_rooms]
+    tier_rooms = [[elsewhere(x, offset, tier == "pinned") for x in mine] for mine in t.tier]
+    tiers = [[r.data_ptr() + offset for r in mine] for mine in tier_rooms]
+    got = [torch.zeros(int(t.cu[-1]) * 2 * D + 8, dtype=torch.bfloat16, device=t.dq.device) for _ in range(2)]
+    torch.cuda.synchronize()
+    t.rebase()
+    t.ctx.kv_load_layer(0, *tiers, *pools)
+    t.ctx.kv_append_save_layer(0, k, v, *pools, *tiers)
+    t.ctx.cached_prefill_attn(0, q, *pools, out, t.scale)
+    t.ctx.kv_read_layer(0, *pools, *(x.data_ptr() + 2 for x in got))
+    t.finish()
+    for room, x in [(rooms[3], t.out)] + list(zip(pool_rooms, t.pools)) + [y for a, b in zip(tier_rooms, t.tier) for y in zip(a, b)]:
+        by = 2 if x is t.out else offset
+        x.reshape(-1).view(torch.uint8).copy_(room[by:by + x.numel() * x.element_size()])
+        assert not room[:by].any() and not room[by + x.numel() * x.element_size():].any()
+    torch.cuda.synchronize()
+    t.check_pools()
+    t.check_tiers()
+    check_rms(t, path)
+    for i in range(2):
+        assert np.array_equal(bf16_bits_to_f64(to_bits(got[i][1:1 + int(t.cu[-1]) * 2 * D])).reshape(-1, 2, D), o4.values(*t.appended[i]))
+
+
 # ---- keys of very different sizes side by side -------------------------------------------------------------------------------------------
 LOW = 8          # rotary pairs of the lowest frequencies, which a few hundred positions hardly turn
 

@@ -1,7 +1,7 @@
-// Causal attention over the 4-bit cache (layout: ca_kv4.h; Sections 2.1, 3.1, 3.4): codes and scales are read, and become bf16 operands
-// of the matrix cores, keys rotated to their rebased positions on the way.  The heads of the queries are normalised first where the
-// layer has a weight for them (x / sqrt(mean(x^2) + eps) * weight), in fp32 and in one pass with the rotation and the scale: the one
-// rounding is to the bf16 operand.
+// Causal attention over the 4-bit cache (layout: ca_kv4.h; Sections 2.1, 3.1, 3.4): codes and scales are read, and become operands of the
+// matrix cores, fp16 keys rotated to their rebased positions on the way, bf16 values.  The heads of the queries are normalised first where
+// the layer has a weight for them (x / sqrt(mean(x^2) + eps) * weight), in fp32.  Here: the kernel for few rows, which rounds queries to fp16
+// and rotates them and the keys in packed fp16; the expansion of the cache; the scalar check kernel.
 #include "ca_kv4.h"
 
 namespace ca {
@@ -42,7 +42,8 @@ __global__ __launch_bounds__(256, 3) void attn_kv4_kernel(AttnArgs a) {
     constexpr int NWV = 4;
     constexpr int PPR = D / 8, KK = D / 32, DB = D / 16, ROWS = kKv4Rows;
     constexpr int KW = D / 64;                 // words of codes of each half of a key that a lane has (2 or 1)
-    constexpr int QSTR = 2 * D + 16;           // row stride of queries, values and angles in LDS (bytes): conflict-free 16-byte accesses
+    constexpr int QSTR = 2 * D + 16;           // row stride of queries, values and angles in LDS (bytes): no conflicts between rows read side by side;
+                                               // half of the kernel's LDS cycles are conflicts all the same, of the values a lane writes 64 bytes apart
     constexpr int OSTR = D + 4;                // of the merge buffer (floats)
     constexpr int VBUF = 32 * QSTR;            // a wavefront's values of one step
     constexpr int SPAN = 64;                   // keys that one rotation of the queries serves
@@ -444,16 +445,18 @@ __global__ __launch_bounds__(256, 3) void attn_kv4_kernel(AttnArgs a) {
     }
 }
 
-// ---- the batch's context as bf16 pages ------------------------------------------------------------------------------------------
-// Keys rotated at their positions, values as they are, into the scratch copies that the kernels over keys rotated beforehand
-// (ca_attn_prerot.hip) read: dense page dp = pool page rot_src_page[dp].  For plans in which many row tiles share the keys of a
+// ---- the batch's context as pages of 16-bit values ------------------------------------------------------------------------------
+// Keys rotated at their positions in fp32, rounded to fp16, values as they are in bf16, into the scratch copies that the kernels over keys
+// rotated beforehand (ca_attn_prerot.hip) read: dense page dp = pool page rot_src_page[dp].  For plans in which many row tiles share the keys of a
 // (conversation, kv head).  Slots past the end of a context become zero (rot_nvalid[dp] of a page are its context's).  Bound by HBM:
 // 17/32 of a byte a value in, two out.  A workgroup has a dense page, a thread one (token, pair of 16-byte pieces) of HEADS heads:
 // the table row is fetched once for all of them and their loads are all in flight.  Measured with 8 kv heads of 128 dims, a grid of
 // 11716 pages: a thread per head 280 us, HEADS 4 196 us (4.9 TB/s, what a copy reaches here); with 4 kv heads of 64 dims only one
 // head is left to a thread.
 // A product of matrix instructions adds 0 x NaN for the keys that a row does not see, so values that are NaN become 0 here and are
-// marked: bit b of v_nan[head][dense page][token] for dims 32 b .. 32 b + 31.  kv4_mark_kernel gives them to the rows that see them.
+// marked: bit b of v_nan[head][dense page][token] for dims 32 b .. 32 b + 31.  mark_nan gives them to the rows that see them.
+// Keys that leave the middle of fp16's range (key_shift in ca_attn_kv4_tiles.hip; zeros do not) are marked too, eight together, and the items
+// that load one are left to the kernel that knows a power of two for every key.
 template <int D, int STYLE, int HEADS>
 __global__ __launch_bounds__(256) void kv4_expand_kernel(AttnArgs a) {
     constexpr int HALF = D / 2, PAIRS = D / 16, SIDE = 256 / (kPageSize * PAIRS);        // heads side by side
@@ -489,6 +492,14 @@ __global__ __launch_bounds__(256) void kv4_expand_kernel(AttnArgs a) {
 #pragma unroll
             for (int b = 0; b < D / 32; ++b) bad |= kv4_is_nan(ve[i] >> 8 * b & 255u) ? 1u << b : 0u;
         if (pr == 0) a.v_nan[((int64_t)g * a.n_dense_pages + dp) * kPageSize + key] = (uint8_t)bad;
+        const uint32_t most = kv4_most_scale<D>(ke[i]);
+        const uint64_t far = __builtin_amdgcn_ballot_w64(valid && most != 0 && (most < 127 - 10 || most > 127 + 12));
+        static_assert(64 / PAIRS == 8 || 64 / PAIRS == 16, "a wavefront has eight keys of a head, or all sixteen");
+        if (threadIdx.x % 64 == 0) {
+            uint8_t *const to = a.k_far + ((int64_t)g * a.n_dense_pages + dp) * 2;
+            if (PAIRS == 8) to[key / 8] = far != 0;
+            else *reinterpret_cast<uint16_t *>(to) = far != 0;
+        }
         const auto scale_of = [&](uint32_t e, int h) CA_INLINE {
             e = e >> 8 * (pr / 4 + h * (D / 64)) & 255u;
             return kv4_scale(!valid ? 0u : kv4_is_nan(e) ? 255u : e);
@@ -502,12 +513,12 @@ __global__ __launch_bounds__(256) void kv4_expand_kernel(AttnArgs a) {
             const float2 x = pair_f32(w0, s0, w), y = pair_f32(w1, s1, w);
             if (STYLE == 0) {
                 const float2 c0 = cs[2 * w], c1 = cs[2 * w + 1];
-                pl[w] = pack_bf16(x.x * c0.x - y.x * c0.y, x.y * c1.x - y.y * c1.y);
-                ph[w] = pack_bf16(y.x * c0.x + x.x * c0.y, y.y * c1.x + x.y * c1.y);
+                pl[w] = pack_f16(x.x * c0.x - y.x * c0.y, x.y * c1.x - y.y * c1.y);
+                ph[w] = pack_f16(y.x * c0.x + x.x * c0.y, y.y * c1.x + x.y * c1.y);
             } else {
                 const float2 c0 = cs[w], c1 = cs[4 + w];
-                pl[w] = pack_bf16(x.x * c0.x - x.y * c0.y, x.y * c0.x + x.x * c0.y);
-                ph[w] = pack_bf16(y.x * c1.x - y.y * c1.y, y.y * c1.x + y.x * c1.y);
+                pl[w] = pack_f16(x.x * c0.x - x.y * c0.y, x.y * c0.x + x.x * c0.y);
+                ph[w] = pack_f16(y.x * c1.x - y.y * c1.y, y.y * c1.x + y.x * c1.y);
             }
         }
         const int64_t at = to + (int64_t)g * kPageSize * D;
@@ -520,39 +531,6 @@ __global__ __launch_bounds__(256) void kv4_expand_kernel(AttnArgs a) {
             const float scale = kv4_scale(is ? ve[i] >> 8 * b & 255u : 0u);
             const uint32_t word = is ? v[i][h] : 0u;
             *reinterpret_cast<uint4 *>(a.v_t + at + h * HALF) = make_uint4(pair_bf16(word, scale, 0), pair_bf16(word, scale, 1), pair_bf16(word, scale, 2), pair_bf16(word, scale, 3));
-        }
-    }
-}
-
-// NaN into the blocks of the output rows that see a value marked by kv4_expand_kernel: a workgroup looks through the marks of a
-// (conversation, kv head) for the first key of each block.  5 us behind an attention of 110 (latency).
-template <int D>
-__global__ __launch_bounds__(256) void kv4_mark_kernel(AttnArgs a) {
-    constexpr int BLOCKS = D / 32;
-    __shared__ int first[BLOCKS];
-    const int c = blockIdx.x / a.n_kv_heads, g = blockIdx.x % a.n_kv_heads, G = a.n_q_heads / a.n_kv_heads;
-    const int n = a.n_keep[c], q0 = a.cu_q[c], len = a.cu_q[c + 1] - q0;
-    if (len == 0) return;
-    if (threadIdx.x < BLOCKS) first[threadIdx.x] = INT_MAX;
-    __syncthreads();
-    const uint4 *const marks = reinterpret_cast<const uint4 *>(a.v_nan) + (int64_t)g * a.n_dense_pages + a.dense_page0[c];
-    const int pages = (n + len + kPageSize - 1) / kPageSize;
-#pragma unroll 4
-    for (int p = threadIdx.x; p < pages; p += 256) {
-        const uint4 m = marks[p];
-        if ((m.x | m.y | m.z | m.w) == 0) continue;
-        const uint32_t word[4] = {m.x, m.y, m.z, m.w};
-        for (int t = 0; t < kPageSize; ++t)
-            for (int b = 0; b < BLOCKS; ++b)
-                if (word[t / 4] >> (8 * (t % 4) + b) & 1u) atomicMin(&first[b], p * kPageSize + t);
-    }
-    __syncthreads();
-    for (int b = 0; b < BLOCKS; ++b) {
-        const int from = max(first[b] - n, 0);                   // first new token that sees it
-        if (first[b] == INT_MAX) continue;
-        for (int64_t i = (int64_t)from * G * 4 + threadIdx.x; i < (int64_t)len * G * 4; i += 256) {
-            uint16_t *const row = a.out + ((q0 + i / (4 * G)) * a.n_q_heads + g * G + i / 4 % G) * D;
-            *reinterpret_cast<uint4 *>(row + 32 * b + 8 * (i % 4)) = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
         }
     }
 }
@@ -660,20 +638,10 @@ hipError_t launch_attn_kv4(const AttnArgs &a, hipStream_t stream) {
 
 hipError_t launch_kv4_expand(const AttnArgs &a, hipStream_t stream) {
     if (a.n_dense_pages <= 0) return hipSuccess;
-    if (!a.k_rot || !a.v_t || !a.v_nan || !a.rot_src_page || !a.rot_pos0 || !a.rot_nvalid) return hipErrorInvalidValue;
+    if (!a.k_rot || !a.v_t || !a.v_nan || !a.k_far || !a.rot_src_page || !a.rot_pos0 || !a.rot_nvalid) return hipErrorInvalidValue;
     return a.head_dim == 128 ? (a.rope_style == 0 ? launch_expand<128, 0>(a, stream) : launch_expand<128, 1>(a, stream))
            : a.head_dim == 64 ? (a.rope_style == 0 ? launch_expand<64, 0>(a, stream) : launch_expand<64, 1>(a, stream))
                               : hipErrorInvalidValue;
-}
-
-hipError_t launch_kv4_mark(const AttnArgs &a, int n_seqs, hipStream_t stream) {
-    if (n_seqs <= 0 || a.n_dense_pages <= 0) return hipSuccess;
-    if (!a.v_nan || !a.dense_page0) return hipErrorInvalidValue;
-    const dim3 grid((uint32_t)n_seqs * (uint32_t)a.n_kv_heads);
-    if (a.head_dim == 128) hipLaunchKernelGGL(kv4_mark_kernel<128>, grid, dim3(256), 0, stream, a);
-    else if (a.head_dim == 64) hipLaunchKernelGGL(kv4_mark_kernel<64>, grid, dim3(256), 0, stream, a);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
 }
 
 hipError_t launch_attn_kv4_ref(const AttnArgs &a, hipStream_t stream) {

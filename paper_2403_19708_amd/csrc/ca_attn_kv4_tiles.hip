@@ -5,8 +5,8 @@
 // a lane owns a query row).  Tiles of 256 rows: 32 rows to a wavefront.  Of 128 (SPLIT): two wavefronts have the same rows and half of each
 // tile's keys, and add up their sums at the end.  The codes of a tile are asked for a tile ahead, into registers (five or six a thread),
 // and tile T + 1 is converted beside the products of tile T (two buffers, one barrier a tile); a workgroup has a compute unit to
-// itself, but two of 128 rows with heads of 64 share one (128 registers a thread, which costs a spilled address or none: 221 -> 175 us for
-// 16 first turns of 128-2048 tokens, 32/4 heads).
+// itself, but two of 128 rows with heads of 64 share one (128 registers a thread, none of them spilled: 221 -> 175 us for 16 first turns of
+// 128-2048 tokens, 32/4 heads).
 //
 // Roundings: queries rotated in fp32 to fp16, eleven bits; keys rotated in packed fp16 with angles in fp16; values not at all (two significant
 // bits); probabilities to bf16, of which the denominator sums what the product uses.  Relative error against 64 bits 0.0022, half of that
@@ -26,6 +26,7 @@
 // it; values that are NaN are left out of the product and put into the rows that see them afterwards.
 #include "ca_kv4.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace ca {
@@ -51,7 +52,7 @@ __device__ CA_INLINE inline void words_from(const uint8_t *at, uint32_t (&to)[W]
 }
 
 template <int D, int STYLE, bool SPLIT>
-__global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_kernel(AttnArgs a) {
+__device__ CA_INLINE inline void attn_kv4_tiles(const AttnArgs &a, const WorkItem &item) {
     constexpr int NW = 8, BN = 64, KSTEPS = D / 16, DBLKS = D / 32;
     constexpr int GROUPS = SPLIT ? NW / 2 : NW;      // of 32 rows
     constexpr int MB = SPLIT ? 1 : 2;                // blocks of 32 keys of a tile that a wavefront multiplies
@@ -73,9 +74,6 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
     };
     __shared__ __attribute__((aligned(16))) Flags flags[2];
     __shared__ float q_up[32 * GROUPS];              // factors of the rows of the queries
-
-    const WorkItem item = a.items[blockIdx.x];
-    if (item.seq < 0) return;
 
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -415,6 +413,69 @@ __global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_
     }
 }
 
+template <int D, int STYLE, bool SPLIT>
+__global__ __launch_bounds__(512, SPLIT && D == 64 ? 4 : 2) void attn_kv4_tiles_kernel(AttnArgs a) {
+    const WorkItem item = a.items[blockIdx.x];
+    if (item.seq >= 0) attn_kv4_tiles<D, STYLE, SPLIT>(a, item);
+}
+
+// ---- behind the attention over the expanded cache (ca_attn_prerot.hip) -------------------------------------------------------------
+// NaN into the blocks of the output rows that see a value marked by kv4_expand_kernel: a workgroup looks through the marks of a
+// (conversation, kv head) for the first key of each block.
+template <int D>
+__device__ inline void mark_nan(const AttnArgs &a, int unit, int (&first)[D / 32]) {
+    constexpr int BLOCKS = D / 32;
+    const int c = unit / a.n_kv_heads, g = unit % a.n_kv_heads, G = a.n_q_heads / a.n_kv_heads, n_threads = blockDim.x;
+    const int n = a.n_keep[c], q0 = a.cu_q[c], len = a.cu_q[c + 1] - q0;
+    __syncthreads();                                             // (of the unit before)
+    if (threadIdx.x < BLOCKS) first[threadIdx.x] = INT_MAX;
+    __syncthreads();
+    const uint4 *const marks = reinterpret_cast<const uint4 *>(a.v_nan) + (int64_t)g * a.n_dense_pages + a.dense_page0[c];
+    const int pages = (n + len + kPageSize - 1) / kPageSize;
+#pragma unroll 4
+    for (int p = threadIdx.x; p < pages; p += n_threads) {
+        const uint4 m = marks[p];
+        if ((m.x | m.y | m.z | m.w) == 0) continue;
+        const uint32_t word[4] = {m.x, m.y, m.z, m.w};
+        for (int t = 0; t < kPageSize; ++t)
+            for (int b = 0; b < BLOCKS; ++b)
+                if (word[t / 4] >> (8 * (t % 4) + b) & 1u) atomicMin(&first[b], p * kPageSize + t);
+    }
+    __syncthreads();
+    for (int b = 0; b < BLOCKS; ++b) {
+        const int from = max(first[b] - n, 0);                   // first new token that sees it
+        if (first[b] == INT_MAX) continue;
+        for (int64_t i = (int64_t)from * G * 4 + threadIdx.x; i < (int64_t)len * G * 4; i += n_threads) {
+            uint16_t *const row = a.out + ((q0 + i / (4 * G)) * a.n_q_heads + g * G + i / 4 % G) * D;
+            *reinterpret_cast<uint4 *>(row + 32 * b + 8 * (i % 4)) = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+        }
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void kv4_mark_kernel(AttnArgs a) {
+    __shared__ int first[D / 32];
+    mark_nan<D>(a, blockIdx.x, first);
+}
+
+// The items that it has left, because of a key or a query outside the middle of fp16's range: a workgroup looks at 64 of them at a time and
+// there is none, as a rule.  Where no shares are merged in between, also the marks of n_units (conversation, kv head); a row that both
+// write gets NaN from either.
+template <int D, int STYLE, bool SPLIT>
+__global__ __launch_bounds__(512, 2) void attn_kv4_rest_kernel(AttnArgs a, int n_units) {
+    __shared__ int first[D / 32];
+    for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x) mark_nan<D>(a, unit, first);
+    for (int from = blockIdx.x; from < a.n_items; from += 64 * gridDim.x) {
+        const int at = from + (int)(threadIdx.x & 63) * (int)gridDim.x;
+        const bool mine = at < a.n_items && a.items[at].seq >= 0 && a.rest[at] != 0;
+        for (uint64_t left = __builtin_amdgcn_ballot_w64(mine); left; left &= left - 1) {
+            const WorkItem item = a.items[from + __builtin_ctzll(left) * (int)gridDim.x];
+            __syncthreads();                                     // (the wavefronts are through with the item before)
+            attn_kv4_tiles<D, STYLE, SPLIT>(a, item);
+        }
+    }
+}
+
 }  // namespace
 
 hipError_t launch_attn_kv4_tiles(const AttnArgs &a, hipStream_t stream) {
@@ -429,6 +490,26 @@ hipError_t launch_attn_kv4_tiles(const AttnArgs &a, hipStream_t stream) {
     hipLaunchKernelGGL(a.tile_rows == 128 ? pick(std::true_type{}) : pick(std::false_type{}), dim3(a.n_items), dim3(512), 0, stream, a);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess || a.n_combine <= 0 ? e : launch_combine_tiles(a, stream);
+}
+
+hipError_t launch_attn_kv4_rest(const AttnArgs &a, int n_seqs, int n_cus, hipStream_t stream) {
+    if (a.n_items <= 0 || n_seqs <= 0) return hipSuccess;
+    if (!a.rope16 || (a.tile_rows != 128 && a.tile_rows != 256) || !a.rest || !a.v_nan || !a.dense_page0 || (a.n_combine > 0 && (!a.partial || !a.combine)))
+        return hipErrorInvalidValue;
+    if (a.head_dim != 128 && a.head_dim != 64) return hipErrorInvalidValue;
+    const auto pick = [&](auto split) {
+        constexpr bool S = decltype(split)::value;
+        return a.head_dim == 128 ? (a.rope_style == 0 ? attn_kv4_rest_kernel<128, 0, S> : attn_kv4_rest_kernel<128, 1, S>)
+                                 : (a.rope_style == 0 ? attn_kv4_rest_kernel<64, 0, S> : attn_kv4_rest_kernel<64, 1, S>);
+    };
+    const int n_units = n_seqs * a.n_kv_heads, marked = a.n_combine > 0 ? 0 : n_units;
+    hipLaunchKernelGGL(a.tile_rows == 128 ? pick(std::true_type{}) : pick(std::false_type{}), dim3(std::min(std::max(a.n_items, marked), n_cus)), dim3(512), 0, stream, a, marked);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.n_combine <= 0) return e;
+    e = launch_combine_tiles(a, stream);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(a.head_dim == 128 ? kv4_mark_kernel<128> : kv4_mark_kernel<64>, dim3(n_units), dim3(256), 0, stream, a);
+    return hipGetLastError();
 }
 
 }  // namespace ca

@@ -26,6 +26,8 @@ namespace {
 
 #define CA_INLINE __attribute__((always_inline))   // (a lambda left as a function keeps the kernel's registers in memory)
 
+typedef __attribute__((ext_vector_type(8))) _Float16 half8;
+
 // Instruction kinds of __builtin_amdgcn_sched_group_barrier
 constexpr int kMfma = 0x008, kVector = 0x402 /* plain and transcendental */, kLdsRead = 0x100;
 
@@ -33,9 +35,11 @@ constexpr int kMaxPagesLds = 2048;   // page ids kept in LDS at a time: a window
 
 // NW wavefronts (32 stacked query rows each) per workgroup, key tiles of BN.  Two shapes are built: NW = 8, BN = 64 (256-row
 // tiles, one workgroup per compute unit) and NW = 4, BN = 32 (128-row tiles, several independent workgroups).
-// OCC = wavefronts per SIMD the register budget is cut for.  NORM: heads of the queries are normalised (q_weight); 20 us of 1800 for 64
-// conversations of 1024-4096 + 64-512 tokens, 64/8 heads, where a pass of its own in front took 88.
-template <int D, int STYLE, int NW, int BN, int OCC, bool NORM>
+// OCC = wavefronts per SIMD the register budget is cut for.  F16: over the expanded 4-bit cache, keys and queries in fp16, which has three bits more
+// than bf16 and costs 3 to 4 % (64 conversations of 1024-4096 + 64-512 tokens, 64/8 heads, 1818 -> 1895 us, error against 64 bits 0.0034 ->
+// 0.0024); an item that loads a key or has a query row outside the middle of its range is left to attn_kv4_rest_kernel.  NORM: heads of
+// the queries are normalised (q_weight); 20 us of those, where a pass of its own in front took 88.
+template <int D, int STYLE, int NW, int BN, int OCC, bool F16, bool NORM>
 __device__ CA_INLINE inline void attn_prerot(const AttnArgs &a) {
     // PIPE: the scores of tile T+1 are formed under the softmax of tile T.  TWO: wavefronts w and w + 4, which share a SIMD,
     // are half a tile apart: one has its second product while the other has first product and softmax.  With heads of 64
@@ -62,14 +66,14 @@ __device__ CA_INLINE inline void attn_prerot(const AttnArgs &a) {
     // iterations whose loads may still be in flight at the end of one: only its own, and where the next one needs nothing
     // but tile T+1 those of the one before as well
     constexpr int FLY = PIPE ? 1 : 2;
-    constexpr int LDS_LEFT = 160 * 1024 / (OCC * 4 / NW) - (NSK + NSV) * TILE;
+    constexpr int LDS_LEFT = 160 * 1024 / (OCC * 4 / NW) - (NSK + NSV) * TILE - (F16 ? 256 : 0);
     constexpr int PGW = LDS_LEFT / 4 < kMaxPagesLds ? LDS_LEFT / 4 / 64 * 64 : kMaxPagesLds;   // page ids kept in LDS at a time
     static_assert(CHUNKS % NW == 0 && (NC == 1 || NW * KPC % kPageSize == 0), "a wavefront's chunks lie at the same rows of their pages");
     static_assert(PGW >= 16 * PPT, "LDS budget");
 
     __shared__ __attribute__((aligned(16))) uint8_t ring_k[NSK * TILE];
     __shared__ __attribute__((aligned(16))) uint8_t ring_v[NSV * TILE];
-    __shared__ int32_t pg[PGW];
+    __shared__ int32_t pg[PGW + (F16 ? 1 : 0)];              // (F16: and whether the item is left)
 
     const WorkItem item = a.items[blockIdx.x];
     if (item.seq < 0) return;
@@ -100,6 +104,12 @@ __device__ CA_INLINE inline void attn_prerot(const AttnArgs &a) {
     const int n_pages = (kmax + kPageSize - 1) / kPageSize;
     int pg_base = t_begin * PPT;
     for (int i = tid; i < min(PGW, n_pages - pg_base); i += NTHREADS) pg[i] = table[pg_base + i];
+    uint32_t far_keys = 0;               // F16: among the pages that the item loads
+    if (F16) {
+        const uint16_t *const marks = reinterpret_cast<const uint16_t *>(a.k_far) + (int64_t)g * a.n_dense_pages + a.dense_page0[c];
+        for (int i = pg_base + tid; i < n_pages; i += NTHREADS) far_keys |= marks[i];
+        if (tid == 0) pg[PGW] = 0;
+    }
 
     // ---- this lane's query row --------------------------------------------------------------
     const int r_raw = item.row0 + wave * 32 + lq;
@@ -197,7 +207,7 @@ __device__ CA_INLINE inline void attn_prerot(const AttnArgs &a) {
 
     // ---- prologue ---------------------------------------------------------------------------------------
     // the queries are asked for before the page ids arrive, and rotated behind the loads of the first tiles
-    QueryRows<D, STYLE, NORM> rows;
+    QueryRows<D, STYLE, F16, NORM> rows;
     if (wave_live) rows.fetch(a, q0, g, G, n, item.row0 + wave * 32, row_last);
     __syncthreads();                     // page ids are in LDS
 #pragma unroll
@@ -212,8 +222,14 @@ __device__ CA_INLINE inline void attn_prerot(const AttnArgs &a) {
     if (wave_live)
         rows.finish((wave / QPT < 2 ? stage_k(t_begin + 2 + wave / QPT) : stage_v(t_begin + wave / QPT)) + wave % QPT * QueryRows<D, STYLE>::kQueryBytes,
                     cscale, Qf);
+    if (F16 && ((wave_live && rows.far()) || __builtin_amdgcn_ballot_w64(far_keys != 0) != 0)) pg[PGW] = 1;
     CA_WAIT_VMCNT(0);
     __syncthreads();
+    if (F16) {
+        const bool leave = __builtin_amdgcn_readfirstlane(pg[PGW]) != 0;
+        if (tid == 0) a.rest[blockIdx.x] = leave;
+        if (leave) return;
+    }
     // what may stay in flight when the walk begins
     if (t_begin + KA - 1 < n_tiles) issue(t_begin + KA - 1, std::false_type{});
     if (t_begin + VA - 1 < n_tiles) issue(t_begin + VA - 1, std::true_type{});
@@ -227,7 +243,8 @@ __device__ CA_INLINE inline void attn_prerot(const AttnArgs &a) {
     auto score_step = [&](f32x16 (&S)[MB], const uint8_t *st, int ks) CA_INLINE {
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-            S[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks % KD][mb], Qf[ks], ks == 0 ? neg_ref : S[mb], 0, 0, 0);
+            if (F16) S[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, kf[ks % KD][mb]), __builtin_bit_cast(half8, Qf[ks]), ks == 0 ? neg_ref : S[mb], 0, 0, 0);
+            else S[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks % KD][mb], Qf[ks], ks == 0 ? neg_ref : S[mb], 0, 0, 0);
         }
         if (ks + KD < KSTEPS) key_step(st, ks + KD);
     };
@@ -521,9 +538,9 @@ __global__ __launch_bounds__(D) void rotate_keys_kernel(AttnArgs a) {
 }
 
 template <int D, int STYLE, int NW, int BN, int OCC>
-__global__ __launch_bounds__(64 * NW, OCC) void attn_prerot_kernel(AttnArgs a) { attn_prerot<D, STYLE, NW, BN, OCC, false>(a); }
-template <int D, int STYLE, int NW, int BN, int OCC>
-__global__ __launch_bounds__(64 * NW, OCC) void attn_prerot_norm_kernel(AttnArgs a) { attn_prerot<D, STYLE, NW, BN, OCC, true>(a); }
+__global__ __launch_bounds__(64 * NW, OCC) void attn_prerot_kernel(AttnArgs a) { attn_prerot<D, STYLE, NW, BN, OCC, false, false>(a); }
+template <int D, int STYLE, int NW, int BN, int OCC, bool NORM>
+__global__ __launch_bounds__(64 * NW, OCC) void attn_prerot_kv4_kernel(AttnArgs a) { attn_prerot<D, STYLE, NW, BN, OCC, true, NORM>(a); }
 
 template <int D, int STYLE>
 void launch_all(const AttnArgs &a, hipStream_t stream) {
@@ -533,10 +550,15 @@ void launch_all(const AttnArgs &a, hipStream_t stream) {
     else if (heads == 4) hipLaunchKernelGGL((rotate_keys_kernel<D, STYLE, 4>), rgrid, dim3(D), 0, stream, a);
     else if (heads == 2) hipLaunchKernelGGL((rotate_keys_kernel<D, STYLE, 2>), rgrid, dim3(D), 0, stream, a);
     else hipLaunchKernelGGL((rotate_keys_kernel<D, STYLE, 1>), rgrid, dim3(D), 0, stream, a);
-    const bool norm = a.q_weight != nullptr;
-    if (a.tile_rows == 256) hipLaunchKernelGGL((norm ? attn_prerot_norm_kernel<D, STYLE, 8, 64, 2> : attn_prerot_kernel<D, STYLE, 8, 64, 2>), grid, dim3(512), 0, stream, a);
-    else if (D == 64 && a.wgs_per_cu == 4) hipLaunchKernelGGL((norm ? attn_prerot_norm_kernel<D, STYLE, 4, 32, D == 64 ? 4 : 2> : attn_prerot_kernel<D, STYLE, 4, 32, D == 64 ? 4 : 2>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((norm ? attn_prerot_norm_kernel<D, STYLE, 4, 32, D == 64 ? 3 : 2> : attn_prerot_kernel<D, STYLE, 4, 32, D == 64 ? 3 : 2>), grid, dim3(256), 0, stream, a);
+    const auto pick = [&](auto nw, auto bn, auto occ) {
+        constexpr int NW = decltype(nw)::value, BN = decltype(bn)::value, OCC = decltype(occ)::value;
+        return !a.expanded ? attn_prerot_kernel<D, STYLE, NW, BN, OCC>
+               : a.q_weight ? attn_prerot_kv4_kernel<D, STYLE, NW, BN, OCC, true> : attn_prerot_kv4_kernel<D, STYLE, NW, BN, OCC, false>;
+    };
+    typedef std::integral_constant<int, 4> four;
+    if (a.tile_rows == 256) hipLaunchKernelGGL(pick(std::integral_constant<int, 8>{}, std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{}), grid, dim3(512), 0, stream, a);
+    else if (D == 64 && a.wgs_per_cu == 4) hipLaunchKernelGGL(pick(four{}, std::integral_constant<int, 32>{}, std::integral_constant<int, D == 64 ? 4 : 2>{}), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL(pick(four{}, std::integral_constant<int, 32>{}, std::integral_constant<int, D == 64 ? 3 : 2>{}), grid, dim3(256), 0, stream, a);
 }
 
 }  // namespace
@@ -546,13 +568,14 @@ hipError_t launch_attn_prerot(const AttnArgs &a, hipStream_t stream) {
     if (a.n_combine > 0 && (a.partial == nullptr || a.combine == nullptr)) return hipErrorInvalidValue;
     if ((a.tile_rows != 256 && a.tile_rows != 128) || !a.k_rot || !a.dense_page0 || !a.rot_src_page || !a.rot_pos0 || a.n_dense_pages <= 0)
         return hipErrorInvalidValue;
+    if (a.expanded && (!a.k_far || !a.rest)) return hipErrorInvalidValue;
     if (a.head_dim == 128 && a.rope_style == 0) launch_all<128, 0>(a, stream);
     else if (a.head_dim == 128) launch_all<128, 1>(a, stream);
     else if (a.head_dim == 64 && a.rope_style == 0) launch_all<64, 0>(a, stream);
     else if (a.head_dim == 64) launch_all<64, 1>(a, stream);
     else return hipErrorInvalidValue;
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.n_combine <= 0) return e;
+    if (e != hipSuccess || a.n_combine <= 0 || a.expanded) return e;
     return launch_combine_tiles(a, stream);
 }
 

@@ -193,8 +193,9 @@ __device__ __attribute__((always_inline)) inline float head_norm(float (&x)[N], 
 // the lines of eight wavefronts that long: 10.6 us from the start of a workgroup of 256 rows to its first tile (32 heads, one
 // row per position).  Here D / 4 lanes fetch a row and its table row side by side, two rotary pairs each, and the rotated row goes
 // through LDS to the lanes that want it.  `fetch` only asks for the data; `finish` needs stage(): kQueryBytes of LDS that nobody else uses.
-// NORM: heads are normalised first, x / sqrt(mean(x^2) + eps) * weight, in fp32.
-template <int D, int STYLE, bool NORM = false>
+// NORM: heads are normalised first, x / sqrt(mean(x^2) + eps) * weight, in fp32.  F16: rounded to fp16; far() then says whether some row's largest
+// value leaves the middle of that range (below 2^11, and 2^-6 or more unless all are zero).
+template <int D, int STYLE, bool F16 = false, bool NORM = false>
 struct QueryRows {
     static constexpr int kStride = 2 * D + 16;             // bytes of a row in LDS: 16-byte reads of 32 rows are free of bank conflicts
     static constexpr int kQueryBytes = 32 * kStride;
@@ -205,6 +206,14 @@ struct QueryRows {
     uint32_t x[STEPS], y[STEPS];
     float gain[4];                                         // NORM: weights of this lane's dims
     float eps;
+    float large;                                           // F16: the largest value of this lane, before the rotation
+    uint64_t small;                                        // F16: rows with values but none of 2^-6
+    // the last lane of every row that has one of `lanes`
+    __device__ static inline uint64_t rows_of(uint64_t lanes) {
+        constexpr uint64_t kLast = LPR == 32 ? 0x8000000080000000ull : 0x8000800080008000ull;
+        return (((lanes & ~kLast) + ~kLast) | lanes) & kLast;
+    }
+    __device__ inline bool far() const { return __builtin_amdgcn_ballot_w64(large >= 0x1p11f) != 0 || small != 0; }
 
     __device__ inline void fetch(const AttnArgs &a, int q0, int g, int G, int n, int row_first, int row_last) {
         const int lane = threadIdx.x & 63, c = lane % LPR;
@@ -239,16 +248,26 @@ struct QueryRows {
         for (int i = 0; i < STEPS; ++i) {
             const float2 first = make_float2(cs[i].x, cs[i].y), second = make_float2(cs[i].z, cs[i].w);
             const float2 both[8] = {first, second, first, second, second, second, second, second};
-            if (NORM) {
+            static_assert(F16 || !NORM, "");
+            if (F16) {
+                typedef __attribute__((ext_vector_type(2))) _Float16 half2v;
+                const auto pack = [](float lo, float hi) { return __builtin_bit_cast(uint32_t, half2v{(_Float16)lo, (_Float16)hi}); };
                 float of[4] = {bf_lo(x[i]), bf_hi(x[i]), bf_lo(y[i]), bf_hi(y[i])};
-                const float inv = f * head_norm<D, LPR>(of, eps);
-                const float u0 = of[0] * inv * gain[0], u1 = of[1] * inv * gain[1], v0 = of[2] * inv * gain[2], v1 = of[3] * inv * gain[3];
+                const float inv = NORM ? f * head_norm<D, LPR>(of, eps) : f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) of[k] *= NORM ? inv * gain[k] : inv;
+                const float u0 = of[0], u1 = of[1], v0 = of[2], v1 = of[3];
+                const float most = fmaxf(fmaxf(fabsf(u0), fabsf(u1)), fmaxf(fabsf(v0), fabsf(v1)));
+                // (without branches: of the lanes with something and those with enough, the lowest of each row by a carry through the row)
+                large = fmaxf(i == 0 ? 0.f : large, most);
+                const uint64_t any = __builtin_amdgcn_ballot_w64(most > 0.f), fine = __builtin_amdgcn_ballot_w64(most >= 0x1p-6f);
+                small = (i == 0 ? 0 : small) | (rows_of(any) & ~rows_of(fine));
                 if (STYLE == 0) {                                // pairs (u0, v0), (u1, v1)
-                    x[i] = pack_bf16(u0 * first.x - v0 * first.y, u1 * second.x - v1 * second.y);
-                    y[i] = pack_bf16(v0 * first.x + u0 * first.y, v1 * second.x + u1 * second.y);
+                    x[i] = pack(u0 * first.x - v0 * first.y, u1 * second.x - v1 * second.y);
+                    y[i] = pack(v0 * first.x + u0 * first.y, v1 * second.x + u1 * second.y);
                 } else {
-                    x[i] = pack_bf16(u0 * first.x - u1 * first.y, u1 * first.x + u0 * first.y);
-                    y[i] = pack_bf16(v0 * second.x - v1 * second.y, v1 * second.x + v0 * second.y);
+                    x[i] = pack(u0 * first.x - u1 * first.y, u1 * first.x + u0 * first.y);
+                    y[i] = pack(v0 * second.x - v1 * second.y, v1 * second.x + v0 * second.y);
                 }
             } else {
                 rotate_dword<STYLE>(x[i], y[i], both, 0, f);     // (STYLE 0: pairs both[0], both[1]; 1: both[0], both[4])

@@ -191,8 +191,10 @@ struct AttnArgs {
     const uint16_t *rope16;      // fp16 [rows of `rope`][4][cos, sin][head_dim/8]: rotary pairs in the order of launch_attn_kv4's lanes
     const uint16_t *q_weight;    // [head_dim] bf16, or null: heads of the queries are not normalised
     float norm_eps;
-    int32_t expanded;            // launch_attn_prerot: the scratch copy of the keys is written already
+    int32_t expanded;            // launch_attn_prerot: over the scratch copies of launch_kv4_expand, in fp16 (and the shares are not merged)
     uint8_t *v_nan;              // [n_kv_heads][n_dense_pages][16] blocks of 32 values that are NaN in the pool and zero in the scratch copy
+    uint8_t *k_far;              // [n_kv_heads][n_dense_pages][2] eights of keys among which one is too large or small for the scratch copy
+    uint8_t *rest;               // [n_items] items that the kernel over expanded keys has left to the one that reads the pool
 };
 
 constexpr int kAttnTileRowsMin = 128;   // smallest tile of stacked query rows (4 wavefronts x 32)
@@ -222,10 +224,11 @@ hipError_t launch_attn_rows(const AttnArgs &args, int wavefronts, bool runs, hip
 hipError_t launch_attn_kv4(const AttnArgs &args, hipStream_t stream);
 // the same for tiles of 128 or 256 rows, work list and merge of the tile kernels (items, combine)
 hipError_t launch_attn_kv4_tiles(const AttnArgs &args, hipStream_t stream);
-// the batch's context -> k_rot (rotated) and v_t (as it is), dense pages in bf16
+// the batch's context -> k_rot (rotated, in fp16) and v_t (as it is, in bf16), dense pages
 hipError_t launch_kv4_expand(const AttnArgs &args, hipStream_t stream);
-// their values that are NaN, into the rows that see them (after the attention)
-hipError_t launch_kv4_mark(const AttnArgs &a, int n_seqs, hipStream_t stream);
+// behind launch_attn_prerot over them: the items it has left (args as for launch_attn_kv4_tiles), the merge of all shares, and values that are
+// NaN into the rows that see them
+hipError_t launch_attn_kv4_rest(const AttnArgs &args, int n_seqs, int n_cus, hipStream_t stream);
 hipError_t launch_attn_kv4_ref(const AttnArgs &args, hipStream_t stream);
 constexpr int kAttnMaxParts = 1024;           // shares of split row tiles per batch (sizes the partial-result buffer)
 constexpr int kAttnMaxPartsPerTile = 16;

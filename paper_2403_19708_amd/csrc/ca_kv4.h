@@ -64,6 +64,8 @@ __device__ __attribute__((always_inline)) inline uint32_t pair_bf16(uint32_t w, 
 typedef __attribute__((ext_vector_type(2))) _Float16 half2v;
 typedef __attribute__((ext_vector_type(8))) _Float16 half8v;
 
+__device__ inline uint32_t pack_f16(float lo, float hi) { return __builtin_bit_cast(uint32_t, half2v{(_Float16)lo, (_Float16)hi}); }
+
 __device__ __attribute__((always_inline)) inline half2v pair_f16(uint32_t w, float scale, int i) {
     switch (i) {
         case 0: return __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0));
@@ -137,17 +139,16 @@ __device__ __attribute__((always_inline)) inline float query_pieces(const AttnAr
             u[i] = __builtin_ldexpf(u[i], -up);
             v[i] = __builtin_ldexpf(v[i], -up);
         }
-    const auto pack = [](float lo, float hi) { return __builtin_bit_cast(uint32_t, half2v{(_Float16)lo, (_Float16)hi}); };
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         if (STYLE == 0) {
             const float2 c0 = cs[2 * w], c1 = cs[2 * w + 1];
-            px[w] = pack(u[2 * w] * c0.x - v[2 * w] * c0.y, u[2 * w + 1] * c1.x - v[2 * w + 1] * c1.y);
-            py[w] = pack(v[2 * w] * c0.x + u[2 * w] * c0.y, v[2 * w + 1] * c1.x + u[2 * w + 1] * c1.y);
+            px[w] = pack_f16(u[2 * w] * c0.x - v[2 * w] * c0.y, u[2 * w + 1] * c1.x - v[2 * w + 1] * c1.y);
+            py[w] = pack_f16(v[2 * w] * c0.x + u[2 * w] * c0.y, v[2 * w + 1] * c1.x + u[2 * w + 1] * c1.y);
         } else {
             const float2 c0 = cs[w], c1 = cs[4 + w];
-            px[w] = pack(u[2 * w] * c0.x - u[2 * w + 1] * c0.y, u[2 * w + 1] * c0.x + u[2 * w] * c0.y);
-            py[w] = pack(v[2 * w] * c1.x - v[2 * w + 1] * c1.y, v[2 * w + 1] * c1.x + v[2 * w] * c1.y);
+            px[w] = pack_f16(u[2 * w] * c0.x - u[2 * w + 1] * c0.y, u[2 * w + 1] * c0.x + u[2 * w] * c0.y);
+            py[w] = pack_f16(v[2 * w] * c1.x - v[2 * w + 1] * c1.y, v[2 * w + 1] * c1.x + v[2 * w] * c1.y);
         }
     }
     return __builtin_ldexpf(1.0f, up);

@@ -100,7 +100,7 @@ struct ca_ctx {
     uint16_t *v_t = nullptr;           // values of the batch context transposed once per layer (same pages)
     bool pipelined = false;             // the plan runs the software-pipelined kernel on the two scratch copies
     size_t off_rot_nvalid = 0;
-    uint8_t *v_nan = nullptr;          // marks of the expanded values that are NaN
+    uint8_t *v_nan = nullptr, *k_far = nullptr, *rest = nullptr;       // marks of the expanded cache, see AttnArgs
     size_t k_rot_pages = 0;
     size_t off_dense0 = 0, off_rot_src = 0, off_rot_pos = 0;
     int32_t n_dense_pages = 0;
@@ -853,6 +853,8 @@ void ca_destroy(ca_ctx *ctx) {
     if (ctx->k_rot) (void)hipFree(ctx->k_rot);
     if (ctx->v_t) (void)hipFree(ctx->v_t);
     if (ctx->v_nan) (void)hipFree(ctx->v_nan);
+    if (ctx->k_far) (void)hipFree(ctx->k_far);
+    if (ctx->rest) (void)hipFree(ctx->rest);
     if (ctx->norm_weights) (void)hipFree(ctx->norm_weights);
     if (ctx->d_meta) (void)hipFree(ctx->d_meta);
     if (ctx->h_meta) (void)hipHostFree(ctx->h_meta);
@@ -984,7 +986,11 @@ static ca_status create_impl(ca_ctx *ctx) {
         CA_HIP(ctx, hipMalloc((void **)&ctx->k_rot, ctx->k_rot_pages * (size_t)c.page_size * (size_t)row_bytes(c)));
         if (ctx->kv4 || (c.head_dim == 128 && c.attn_schedule == 1))
             CA_HIP(ctx, hipMalloc((void **)&ctx->v_t, ctx->k_rot_pages * (size_t)c.page_size * (size_t)row_bytes(c)));
-        if (ctx->kv4) CA_HIP(ctx, hipMalloc((void **)&ctx->v_nan, ctx->k_rot_pages * (size_t)c.page_size * (size_t)c.n_kv_heads));
+        if (ctx->kv4) {
+            CA_HIP(ctx, hipMalloc((void **)&ctx->v_nan, ctx->k_rot_pages * (size_t)c.page_size * (size_t)c.n_kv_heads));
+            CA_HIP(ctx, hipMalloc((void **)&ctx->k_far, ctx->k_rot_pages * 2 * (size_t)c.n_kv_heads));
+            CA_HIP(ctx, hipMalloc((void **)&ctx->rest, ctx->items_capacity));
+        }
     }
     if (ctx->kv4) {
         ctx->head_norm.resize(c.n_layers);
@@ -2590,6 +2596,8 @@ static ca_status attn_impl(ca_ctx *ctx, int32_t layer, const void *q, const void
         a.norm_eps = ctx->head_norm[layer].eps;
         a.rope16 = ctx->rope16;
         a.v_nan = ctx->v_nan;
+        a.k_far = ctx->k_far;
+        a.rest = ctx->rest;
         a.kv4_items = (const Kv4Item *)(ctx->d_meta + ctx->off_kv4_items);
         if (!direct) {
             CA_HIP(ctx, launch_attn_kv4_ref(a, stream));
@@ -2599,11 +2607,12 @@ static ca_status attn_impl(ca_ctx *ctx, int32_t layer, const void *q, const void
             CA_HIP(ctx, launch_attn_kv4_tiles(a, stream));
         } else {
             CA_HIP(ctx, launch_kv4_expand(a, stream));
-            a.expanded = 1;
-            a.v_pool = ctx->v_t;
-            a.block_table = (const int32_t *)(ctx->d_meta + ctx->off_dense_table);
-            CA_HIP(ctx, launch_attn_prerot(a, stream));
-            CA_HIP(ctx, launch_kv4_mark(a, ctx->n_seqs, stream));
+            AttnArgs over = a;
+            over.expanded = 1;
+            over.v_pool = ctx->v_t;
+            over.block_table = (const int32_t *)(ctx->d_meta + ctx->off_dense_table);
+            CA_HIP(ctx, launch_attn_prerot(over, stream));
+            CA_HIP(ctx, launch_attn_kv4_rest(a, ctx->n_seqs, ctx->n_cus, stream));
         }
         CA_HIP(ctx, prof_end(ctx, iv, stream));
         return CA_OK;

@@ -20,7 +20,8 @@ SWITCHES = {ROWS: dict(), TILES128: dict(attn_prerotate=1, attn_tile_rows=128), 
 U8, U11 = 2.0 ** -8 * 0.425, 2.0 ** -11 * 0.425
 # Of a rotation in fp16 the angle, a product and the sum are rounded, and the part of the pair that is left out of a component is no larger than
 # the pair: 3 roundings, of up to sqrt(2) of the component.  Queries are rounded before they are rotated (few rows), or behind (tiles), keys not.
-OPERANDS = {ROWS: 2 ** 0.5 * 7 ** 0.5 * U11, TILES128: 2 ** 0.5 * 4 ** 0.5 * U11, TILES256: 2 ** 0.5 * 4 ** 0.5 * U11, EXPANDED: 2 ** 0.5 * U8, SCALAR: 0.0}
+# The expanded path rounds either once, rotated in fp32, and leaves to the tiles what is too large or small for that.
+OPERANDS = {ROWS: 2 ** 0.5 * 7 ** 0.5 * U11, TILES128: 2 ** 0.5 * 4 ** 0.5 * U11, TILES256: 2 ** 0.5 * 4 ** 0.5 * U11, EXPANDED: 2 ** 0.5 * 4 ** 0.5 * U11, SCALAR: 0.0}
 PROBABILITIES = {ROWS: U8, TILES128: U8, TILES256: U8, EXPANDED: U8, SCALAR: 0.0}
 
 
@@ -142,7 +143,7 @@ def test_random_batches(turn, seed):
     t.finish()
     t.check_pools()
     t.check_tiers()
-    check_rms(t, EXPANDED)                                           # the loosest of the limits
+    check_rms(t, ROWS)                                               # the loosest of the limits
     t.out.fill_(float("nan"))
     before = t.out.clone()
     t.attend(out=before)

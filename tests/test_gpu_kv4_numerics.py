@@ -253,3 +253,42 @@ def test_norms_of_heads_of_any_size(turn, path, T, Hq, H, D, exponent, eps):
     run(t)
     t.check_pools()
     check_rms(t, path)
+
+
+@pytest.mark.parametrize("D,Hq", [(128, 4), (64, 4)])
+@pytest.mark.parametrize("bad", [False, True])
+def test_shares_over_the_expanded_cache_from_both_kernels(turn, D, Hq, bad):
+    """one share of a row tile loads a key outside the middle of fp16's range, the others do not; then a value that is NaN as well"""
+    H, hist, new = 1, 3000, 130
+    t = turn([hist], [new], Hq, H, D, seed=12, **SWITCHES[EXPANDED])
+    k = bf16_bits_to_f64(draw_values_bf16((hist, H, D), 12, 10))
+    v = bf16_bits_to_f64(draw_values_bf16((hist, H, D), 12, 11))
+    low = np.concatenate([np.arange(D // 2 - LOW, D // 2), np.arange(D - LOW, D)])
+    k[100], k[1700] = 0.0, k[1700] * 2.0 ** -30
+    k[100, :, low] = 2.0 ** 30
+    if bad:
+        v[2001, :, 40] = np.nan
+    f = lambda x: (np.asarray(x, np.float32).view(np.uint32) >> 16).astype(np.uint16)
+    q = bf16_bits_to_f64(t.q)
+    q[..., low] = 0.0                                                # its scores are none: among 3000 keys it is one more
+    t.q = f(q)
+    t.dq.copy_(to_torch(t.q))
+    t.saved[0] = [o4.quantise(f(x)) for x in (k, v)]
+    for i in range(2):
+        t.tier[i][0][:hist] = torch.from_numpy(o4.rows(*t.saved[0][i])).to(t.tier[i][0].device)
+    torch.cuda.synchronize()
+    t.rebase()
+    items = t.ctx.rebase_read(6).reshape(-1, 8)
+    assert (items[items[:, 0] >= 0][:, 6] >= 0).any()
+    t.load()
+    t.append()
+    t.attend()
+    t.finish()
+    got = bf16_bits_to_f64(to_bits(t.out))
+    if bad:
+        assert np.isnan(got[:, :, 32:64]).all() and np.isfinite(got[:, :, :32]).all() and np.isfinite(got[:, :, 64:]).all()
+        t.saved[0][1] = o4.quantise(f(np.nan_to_num(v)))             # the other dimensions are those without it
+        clean = t.out.clone()
+        clean[:, :, 32:64] = to_torch(f(np.concatenate([exact(t, 0, 0)[0][:, :, 32:64]]))).reshape(clean[:, :, 32:64].shape)
+        t.out.copy_(clean)
+    check_rms(t, EXPANDED)

@@ -55,6 +55,10 @@
  *   contiguous   per conversation and layer [tokens][row], a row being the token's codes [n_kv_heads][head_dim / 2], then
  *                its scale bytes [n_kv_heads][head_dim / 32], then zeros up to a multiple of 16 bytes (ca_kv_sizes).
  *   q, out and the new turn's keys and values stay bf16.  What is cached has no positional encoding here either.
+ *   attention    rounds queries and keys to fp16 for the score product, probabilities and outputs to bf16, whichever way a plan takes
+ *                (attn_variant 1: only outputs).  A key keeps its bits whatever the other keys hold; inside a key those of blocks
+ *                with less than 2^-10 of its largest block are lost by and by, and in a query those of dimensions with less than
+ *                2^-14 of its largest, below 2^-24 all of them.
  */
 #ifndef CA_H_
 #define CA_H_
@@ -179,8 +183,9 @@ ca_status ca_config_validate_kv4(const ca_config *cfg, char *err, int32_t err_le
 ca_status ca_create(const ca_config *cfg, ca_ctx **out);
 /* The same for the 4-bit cache (see above).  The attention switches keep their meaning, but for two: with attn_tile_rows 0 and
  * attn_prerotate 0 a plan of more than 16 stacked rows takes tiles of 256 rows, tiles of 128, or first expands the batch's context,
- * keys rotated, into bf16 scratch copies of the context's, whichever is estimated to take least.  attn_prerotate 2: all
- * plans expand it; 1: none does, and no scratch copies are allocated.                                                     */
+ * keys rotated, into 16-bit scratch copies of the context's, whichever is estimated to take least (ca_rope_rebase lays out all three:
+ * 84 to 251 us of host time for batches of 8 to 64 turns, where a bf16 context takes 28 to 62).  attn_prerotate 2: all plans
+ * expand it; 1: none does, and no scratch copies are allocated (4 * n_kv_heads * head_dim bytes a token of max_batch_kv_tokens). */
 ca_status ca_create_kv4(const ca_config *cfg, ca_ctx **out);
 void ca_destroy(ca_ctx *ctx);
 /* Bytes of one page (all kv heads) of a pool and of one token in the tier, keys or values, of this context.             */

@@ -1221,8 +1221,8 @@ static ca_status plan_rows(ca_ctx *ctx, size_t &up) {
     return CA_OK;
 }
 
-// us of writing a plan's context over the 4-bit cache to bf16 scratch pages and of marking its NaN values: 4.9 TB/s (what heads of
-// 64 read again of them beside it: 2.5) and two launches more
+// us of writing a plan's context over the 4-bit cache to 16-bit scratch pages and of what follows the attention over them: 4.9 TB/s (what
+// heads of 64 read again of them beside it: 2.5) and two launches more
 static double kv4_expand_time(const ca_ctx *ctx) {
     return 8.0 + (double)ctx->total_k * ctx->cfg.n_kv_heads * ctx->cfg.head_dim * 2 * (2.0 + 17.0 / 32) / (ctx->cfg.head_dim == 64 ? 2.5e6 : 4.9e6);
 }
@@ -1346,8 +1346,7 @@ struct Item { WorkItem w; double cost; int32_t parent; };
 // more than 3 % in 19.  (One layer of 13 conversations of 2134-2392 tokens with 9-45 new ones, 16/8 heads of 64: 38 us in
 // 832 shares, 72 whole.)
 // The 4-bit cache has times of its own, of plans left whole with 64 to 256 rows to a tile and 512 to 8192 tokens of history, and
-// a merge of 3.5 TB/s; before its tile kernel had fp16 keys, with their times, the estimates of nine in ten of 288 plans were 0.79 to 1.07 of
-// what these took, 0.94 in the middle.
+// a merge of 3.5 TB/s.  How the choice by them does: ca_rope_rebase.
 static double plan_time(const ca_ctx *ctx, const std::vector<std::vector<Item>> &plan, const std::vector<int32_t> &parts_of, int bins) {
     struct Times { double tile, tile_alone, item, shares; };
     const bool d64 = ctx->cfg.head_dim == 64, small = ctx->tile_rows == 128;
@@ -1805,12 +1804,13 @@ ca_status ca_rope_rebase(ca_ctx *ctx, const ca_batch *b, void *stream_) {
             if (st != CA_OK) return st;
         } else {
             // The 4-bit cache: tiles of 256 rows or of 128, converting and rotating keys as they read them, or the kernel over expanded
-            // keys behind an expansion of the whole context: whichever plan is estimated to take least.  Of 123 batches (1, 8 and 40
-            // conversations, no history to 3200 tokens, 30 to 800 new, three shapes of heads) all but one take at most 5 % more than the best
-            // of the three, that one 14 % (35 us).  us of the attention by tiles of 256, of 128, and expanded:
-            //   8 of 3000 + 400, 64/8 heads      360, 473, 348        8 of 3000 + 100, 64/8       115, 142, 125
-            //   1 of 3000 + 400, 64/8             85,  83,  91        1 of 1000 + 400, 64/8        51,  41,  53
-            //   40 of 1000 + 400, 32/4 of 64     295, 301, 223        8 of 3000 + 400, 32 heads   222, 262, 342
+            // keys behind an expansion of the whole context: whichever plan is estimated to take least.  Of 150 batches (1, 8 and 40
+            // conversations, no history to 3200 tokens, 30 to 800 new, three shapes of heads) 146 take at most 5 % more than the best of the
+            // three, four of less than 16 us 6 to 12 %.  The layouts are host time, 84 to 251 us a plan for batches of 8 to 64 turns where
+            // the bf16 cache's one takes 28 to 62.  us of the attention by tiles of 256, of 128, and expanded:
+            //   8 of 3000 + 400, 64/8 heads      312, 420, 307        8 of 3000 + 100, 64/8        97, 121, 113
+            //   1 of 3000 + 400, 64/8             77,  74,  86        1 of 1000 + 400, 64/8        47,  36,  49
+            //   40 of 1000 + 400, 32/4 of 64     255, 258, 204        8 of 3000 + 400, 32 heads   187, 219, 323
             struct Way { int tile; bool expanded; };
             Way ways[3];
             int n_ways = 0;
